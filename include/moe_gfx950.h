@@ -290,6 +290,86 @@ int moe_probe_copy(void *dst, const void *src, size_t bytes, float *gbytes_per_s
  * nothing is accessed out of bounds; the output rows of its token are then meaningless).  Synchronises the stream. */
 int moe_last_device_status(const moe_plan_t *plan, const void *workspace, void *hip_stream);
 
+/* --------------------------------------------------------------------------------------------------------------------
+ * Operators around the experts.
+ *
+ * For callers whose experts are not the two products of moe_layer_forward (other layers, other types, training): the row order
+ * of the shared tensor, the dispatch of the tokens into it, the top-k reduction out of it, the norms on either side of the
+ * block, and the gradients of these and of the gate.  Rows are bf16, fp16 or fp32 (moe_dtype_t); sums over them are fp32, each
+ * result is rounded once.  The same call gives the same bits every time.  No plan, and no state between calls: workspaces are
+ * scratch, and calls that may overlap in time need one each.
+ * Supported: T >= 0; 8 <= H <= 65536 (norms: 16384), odd H included; 1 <= k <= 64, E <= 256, T*k < 2^24 (norms: T < 2^24),
+ * T*H*(bytes of an element) < 2^36; anything else is MOE_ERR_UNSUPPORTED.  Row offsets are 64-bit.  With T = 0 the row pointers may be
+ * NULL, and what sums over tokens is written as zeros.  Outputs must not overlap inputs or each other except where said.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef enum { MOE_BF16 = 0, MOE_FP16 = 1, MOE_FP32 = 2 } moe_dtype_t;
+typedef enum { MOE_NORM_RMS = 0, MOE_NORM_LAYER = 1 } moe_norm_t;
+typedef enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2, MOE_GATE_FULL = 3 } moe_gate_t;
+
+/* Row order of the shared tensor: rows grouped by expert, inside an expert in the order of the pair ids q = t*k + j (that of
+ * moe_layer_forward).  topk_ids: dev int32 [T,k]; a value outside [0,E) means that the slot has no expert (a padded token, an
+ * expert of another GPU): it gets no row.  expert_offsets: dev int32 [E+1], rows of expert e are expert_offsets[e] ..
+ * expert_offsets[e+1]-1; perm: dev int32 [T*k], row -> pair id, -1 behind the last row; inv_perm: dev int32 [T,k], pair -> row,
+ * -1 without one.  workspace: dev, >= moe_sort_workspace_bytes (0: such a shape is refused). */
+size_t moe_sort_workspace_bytes(int32_t T, int32_t E, int32_t k);
+int moe_sort_tokens(const int32_t *topk_ids, int32_t T, int32_t E, int32_t k, int32_t *expert_offsets, int32_t *perm,
+                    int32_t *inv_perm, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Dispatch: rows[inv_perm[t,j]] = x[t].  x: dev [T,H]; rows: dev [T*k,H]; rows that no pair has are left as they were.
+ * inv_perm: dev int32 [T,k]; values outside [0,T*k) mean no row, the others must be distinct.
+ * moe_dispatch_backward: grad_x[t] = sum_j grad_rows[inv_perm[t,j]] over the slots that have a row. */
+int moe_dispatch(const void *x, const int32_t *inv_perm, int32_t T, int32_t H, int32_t k, int32_t dtype, void *rows,
+                 void *hip_stream);
+int moe_dispatch_backward(const void *grad_rows, const int32_t *inv_perm, int32_t T, int32_t H, int32_t k, int32_t dtype,
+                          void *grad_x, void *hip_stream);
+
+/* Combine: out[t] = sum_j topk_weights[t,j] * rows[inv_perm[t,j]] over the slots that have a row, in the order of j (0 where
+ * none has).  What lies in rows that no pair has does not matter.  topk_weights: dev fp32 [T,k], NULL: ones.
+ * moe_combine_backward: grad_rows[inv_perm[t,j]] = topk_weights[t,j] * grad_out[t] (other rows are left as they were) and
+ * grad_weights[t,j] = <grad_out[t], rows[inv_perm[t,j]]>, 0 for a slot without a row (dev fp32 [T,k]; NULL: not wanted, rows may
+ * then be NULL). */
+int moe_combine(const void *rows, const int32_t *inv_perm, const float *topk_weights, int32_t T, int32_t H, int32_t k,
+                int32_t dtype, void *out, void *hip_stream);
+int moe_combine_backward(const void *grad_out, const void *rows, const int32_t *inv_perm, const float *topk_weights, int32_t T,
+                         int32_t H, int32_t k, int32_t dtype, void *grad_rows, float *grad_weights, void *hip_stream);
+
+/* Gradient of moe_route_topk's weights with respect to the logits: with sum_t = sum_i grad_weights[t,i] * topk_weights[t,i],
+ * grad_logits[t, topk_ids[t,j]] = topk_weights[t,j] * (grad_weights[t,j] - sum_t), 0 for the experts that were not picked.  A
+ * slot whose id is outside [0,E) takes part in sum_t only; slots with the same id are added up.  grad_logits: dev fp32 [T,E],
+ * written whole. */
+int moe_route_topk_backward(const int32_t *topk_ids, const float *topk_weights, const float *grad_weights, int32_t T, int32_t E,
+                            int32_t k, float *grad_logits, void *hip_stream);
+
+/* In front of the block: s = residual + residual_scale * update, sum = s, x = norm(s) * gamma + beta, with
+ * norm(s) = s / sqrt(mean(s^2) + eps) (MOE_NORM_RMS) or (s - mean(s)) / sqrt(var(s) + eps) (MOE_NORM_LAYER), over the H columns.
+ * x is normed from s before its rounding.  residual, update, sum, x: dev [T,H]; update NULL: s = residual; sum NULL: not wanted.
+ * gamma, beta: dev [H] of the same type; beta NULL: none.  eps >= 0.  sum or x may be residual or update (in place). */
+int moe_norm_before(const void *residual, const void *update, float residual_scale, const void *gamma, const void *beta,
+                    int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void *sum, void *x, void *hip_stream);
+
+/* Its gradient at sum: total = grad_sum + (gradient of the norm for grad_x); grad_residual = total, grad_update =
+ * residual_scale * total (NULL: not wanted), grad_gamma = sum_t grad_x[t] * norm(sum[t]), grad_beta = sum_t grad_x[t] (dev fp32
+ * [H], each NULL: not wanted).  grad_sum: gradient that reaches sum past the block, NULL: none.  grad_residual or grad_update may
+ * be sum, grad_x or grad_sum (in place).  workspace: dev, >= moe_norm_workspace_bytes, for grad_gamma and grad_beta only. */
+size_t moe_norm_workspace_bytes(int32_t T, int32_t H);
+int moe_norm_before_backward(const void *sum, const void *gamma, const void *grad_x, const void *grad_sum, float residual_scale,
+                             int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void *grad_residual, void *grad_update,
+                             float *grad_gamma, float *grad_beta, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Behind the block: out = residual + residual_scale * gate * (norm(y) * gamma + beta).  residual (NULL: 0), y, out: dev [T,H].
+ * gate by gate_kind: MOE_GATE_NONE NULL; MOE_GATE_CHANNEL dev [H] and MOE_GATE_FULL dev [T,H] of the rows' type;
+ * MOE_GATE_TOKEN dev fp32 [T].  out may be residual, y or a full gate (in place).
+ * Its gradient: grad_y; grad_gamma, grad_beta (dev fp32 [H]); grad_gate: dev fp32 [H] or [T] for a channel or token gate, [T,H] of
+ * the rows' type for a full one.  The gradient of residual is grad_out.  All but grad_y may be NULL: not wanted.  grad_y or a full
+ * grad_gate may be y, grad_out or the full gate (in place).  workspace as above, for what is summed over tokens. */
+int moe_norm_after(const void *residual, const void *y, const void *gamma, const void *beta, const void *gate, int32_t gate_kind,
+                   float residual_scale, int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void *out,
+                   void *hip_stream);
+int moe_norm_after_backward(const void *y, const void *gamma, const void *beta, const void *gate, int32_t gate_kind,
+                            float residual_scale, const void *grad_out, int32_t norm, float eps, int32_t T, int32_t H,
+                            int32_t dtype, void *grad_y, float *grad_gamma, float *grad_beta, void *grad_gate, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
 const char *moe_status_string(int status);
 
 #ifdef __cplusplus

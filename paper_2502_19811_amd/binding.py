@@ -11,6 +11,9 @@ from typing import Optional, Sequence
 
 MOE_ACT_GELU = 0
 MOE_ACT_SWIGLU = 1
+MOE_BF16, MOE_FP16, MOE_FP32 = 0, 1, 2
+MOE_NORM_RMS, MOE_NORM_LAYER = 0, 1
+MOE_GATE_NONE, MOE_GATE_CHANNEL, MOE_GATE_TOKEN, MOE_GATE_FULL = 0, 1, 2, 3
 
 _LIB_NAME = "libmoe_gfx950.so"
 _lib = None
@@ -22,6 +25,9 @@ EXPORTS = [
     "moe_status_string", "moe_plan_phase_times", "moe_plan_forward_times", "moe_play_arrival",
     "moe_probe_mfma", "moe_probe_copy", "moe_pack_weights", "moe_layer_forward_static", "moe_get_schedule",
     "moe_plan_schedule_capacity", "moe_probe_mix",
+    "moe_sort_workspace_bytes", "moe_sort_tokens", "moe_dispatch", "moe_dispatch_backward", "moe_combine", "moe_combine_backward",
+    "moe_route_topk_backward", "moe_norm_workspace_bytes", "moe_norm_before", "moe_norm_before_backward", "moe_norm_after",
+    "moe_norm_after_backward",
 ]
 
 
@@ -98,6 +104,24 @@ def load_library():
     lib.moe_play_arrival.restype = C.c_int
     lib.moe_pack_weights.argtypes = [C.c_void_p, vp, vp, vp, vp, vp]
     lib.moe_pack_weights.restype = C.c_int
+    i32, f32, size = C.c_int32, C.c_float, C.c_size_t
+    lib.moe_sort_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.moe_sort_workspace_bytes.restype = size
+    lib.moe_sort_tokens.argtypes = [i32p, i32, i32, i32, i32p, i32p, i32p, vp, size, vp]
+    lib.moe_dispatch.argtypes = [vp, i32p, i32, i32, i32, i32, vp, vp]
+    lib.moe_dispatch_backward.argtypes = [vp, i32p, i32, i32, i32, i32, vp, vp]
+    lib.moe_combine.argtypes = [vp, i32p, f32p, i32, i32, i32, i32, vp, vp]
+    lib.moe_combine_backward.argtypes = [vp, vp, i32p, f32p, i32, i32, i32, i32, vp, f32p, vp]
+    lib.moe_route_topk_backward.argtypes = [i32p, f32p, f32p, i32, i32, i32, f32p, vp]
+    lib.moe_norm_workspace_bytes.argtypes = [i32, i32]
+    lib.moe_norm_workspace_bytes.restype = size
+    lib.moe_norm_before.argtypes = [vp, vp, f32, vp, vp, i32, f32, i32, i32, i32, vp, vp, vp]
+    lib.moe_norm_before_backward.argtypes = [vp, vp, vp, vp, f32, i32, f32, i32, i32, i32, vp, vp, f32p, f32p, vp, size, vp]
+    lib.moe_norm_after.argtypes = [vp, vp, vp, vp, vp, i32, f32, i32, f32, i32, i32, i32, vp, vp]
+    lib.moe_norm_after_backward.argtypes = [vp, vp, vp, vp, i32, f32, vp, i32, f32, i32, i32, i32, vp, f32p, f32p, vp, vp, size, vp]
+    for name in ("moe_sort_tokens", "moe_dispatch", "moe_dispatch_backward", "moe_combine", "moe_combine_backward",
+                 "moe_route_topk_backward", "moe_norm_before", "moe_norm_before_backward", "moe_norm_after", "moe_norm_after_backward"):
+        getattr(lib, name).restype = C.c_int
     lib.moe_status_string.argtypes = [C.c_int]
     lib.moe_status_string.restype = C.c_char_p
     _lib = lib
@@ -266,3 +290,172 @@ def moe_probe_copy(dst, src, stream=None) -> float:
     nbytes = src.numel() * src.element_size()
     _check(load_library().moe_probe_copy(_ptr(dst), _ptr(src), nbytes, C.byref(out), _stream(stream)), "moe_probe_copy")
     return float(out.value)
+
+
+# ---- operators around the experts ----
+# The C calls see addresses only, so what they cannot check is checked here: every tensor has the type and shape its call
+# says, is contiguous, and lies on the current device, as the stream does.
+
+_DTYPES = {"torch.bfloat16": MOE_BF16, "torch.float16": MOE_FP16, "torch.float32": MOE_FP32}
+_INT32, _FLOAT32, _UINT8 = "torch.int32", "torch.float32", "torch.uint8"
+
+
+class _Call:
+    """The tensors of one call: arg() checks one and gives its address."""
+
+    __slots__ = ("where", "device", "stream")
+
+    def __init__(self, where: str, stream):
+        import torch
+        self.where = where
+        self.device = torch.cuda.current_device()
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        elif stream.device_index != self.device:
+            self.refuse()
+        self.stream = stream.cuda_stream
+
+    def refuse(self):
+        raise MoEError(-1, self.where)
+
+    def arg(self, t, dtype: str, *shape) -> int:
+        if str(t.dtype) != dtype or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
+            self.refuse()
+        return t.data_ptr()
+
+    def opt(self, t, dtype: str, *shape) -> Optional[int]:
+        return None if t is None else self.arg(t, dtype, *shape)
+
+    def rows(self, t):
+        """(T, H, type's name, its number) of a tensor of rows."""
+        name = str(t.dtype)
+        if t.dim() != 2 or name not in _DTYPES:
+            self.refuse()
+        return t.shape[0], t.shape[1], name, _DTYPES[name]
+
+    def pairs(self, t):
+        """(T, k) of a tensor of pairs."""
+        if t.dim() != 2:
+            self.refuse()
+        return t.shape
+
+    def workspace(self, t):
+        if t is None:
+            return None, 0
+        return self.arg(t, _UINT8, t.numel()), t.numel()
+
+    def done(self, status: int) -> None:
+        if status != 0:
+            raise MoEError(status, self.where)
+
+
+def moe_sort_workspace_bytes(T: int, E: int, k: int) -> int:
+    return load_library().moe_sort_workspace_bytes(T, E, k)
+
+
+def moe_sort_tokens(topk_ids, E: int, expert_offsets, perm, inv_perm, workspace, stream=None) -> None:
+    """topk_ids int32 [T,k] -> expert_offsets int32 [E+1], perm int32 [T*k], inv_perm int32 [T,k]; workspace uint8."""
+    c = _Call("moe_sort_tokens", stream)
+    T, k = c.pairs(topk_ids)
+    c.done(load_library().moe_sort_tokens(
+        c.arg(topk_ids, _INT32, T, k), T, E, k, c.arg(expert_offsets, _INT32, E + 1), c.arg(perm, _INT32, T * k),
+        c.arg(inv_perm, _INT32, T, k), *c.workspace(workspace), c.stream))
+
+
+def moe_dispatch(x, inv_perm, rows, stream=None) -> None:
+    """x [T,H], inv_perm int32 [T,k] -> rows [T*k,H]."""
+    c = _Call("moe_dispatch", stream)
+    (T, H, name, dtype), k = c.rows(x), c.pairs(inv_perm)[1]
+    c.done(load_library().moe_dispatch(c.arg(x, name, T, H), c.arg(inv_perm, _INT32, T, k), T, H, k, dtype,
+                                       c.arg(rows, name, T * k, H), c.stream))
+
+
+def moe_dispatch_backward(grad_rows, inv_perm, grad_x, stream=None) -> None:
+    """grad_rows [T*k,H], inv_perm int32 [T,k] -> grad_x [T,H]."""
+    c = _Call("moe_dispatch_backward", stream)
+    (T, H, name, dtype), k = c.rows(grad_x), c.pairs(inv_perm)[1]
+    c.done(load_library().moe_dispatch_backward(c.arg(grad_rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), T, H, k, dtype,
+                                                c.arg(grad_x, name, T, H), c.stream))
+
+
+def moe_combine(rows, inv_perm, topk_weights, out, stream=None) -> None:
+    """rows [T*k,H], inv_perm int32 [T,k], topk_weights fp32 [T,k] or None -> out [T,H]."""
+    c = _Call("moe_combine", stream)
+    (T, H, name, dtype), k = c.rows(out), c.pairs(inv_perm)[1]
+    c.done(load_library().moe_combine(c.arg(rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), c.opt(topk_weights, _FLOAT32, T, k),
+                                      T, H, k, dtype, c.arg(out, name, T, H), c.stream))
+
+
+def moe_combine_backward(grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights, stream=None) -> None:
+    """grad_out [T,H], rows [T*k,H] -> grad_rows [T*k,H], grad_weights fp32 [T,k] (None: not wanted, rows may be None)."""
+    c = _Call("moe_combine_backward", stream)
+    (T, H, name, dtype), k = c.rows(grad_out), c.pairs(inv_perm)[1]
+    c.done(load_library().moe_combine_backward(
+        c.arg(grad_out, name, T, H), c.opt(rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), c.opt(topk_weights, _FLOAT32, T, k),
+        T, H, k, dtype, c.arg(grad_rows, name, T * k, H), c.opt(grad_weights, _FLOAT32, T, k), c.stream))
+
+
+def moe_route_topk_backward(topk_ids, topk_weights, grad_weights, grad_logits, stream=None) -> None:
+    """topk_ids int32 [T,k], topk_weights and grad_weights fp32 [T,k] -> grad_logits fp32 [T,E]."""
+    c = _Call("moe_route_topk_backward", stream)
+    (T, k), E = c.pairs(topk_ids), c.pairs(grad_logits)[1]
+    c.done(load_library().moe_route_topk_backward(
+        c.arg(topk_ids, _INT32, T, k), c.arg(topk_weights, _FLOAT32, T, k), c.arg(grad_weights, _FLOAT32, T, k), T, E, k,
+        c.arg(grad_logits, _FLOAT32, T, E), c.stream))
+
+
+def moe_norm_workspace_bytes(T: int, H: int) -> int:
+    return load_library().moe_norm_workspace_bytes(T, H)
+
+
+def moe_norm_before(residual, update, residual_scale: float, gamma, beta, norm: int, eps: float, sum, x, stream=None) -> None:
+    """sum = residual + residual_scale * update, x = norm of it; update, beta and sum may be None."""
+    c = _Call("moe_norm_before", stream)
+    T, H, name, dtype = c.rows(residual)
+    c.done(load_library().moe_norm_before(
+        c.arg(residual, name, T, H), c.opt(update, name, T, H), residual_scale, c.arg(gamma, name, H), c.opt(beta, name, H), norm, eps,
+        T, H, dtype, c.opt(sum, name, T, H), c.arg(x, name, T, H), c.stream))
+
+
+def moe_norm_before_backward(sum, gamma, grad_x, grad_sum, residual_scale: float, norm: int, eps: float, grad_residual, grad_update,
+                             grad_gamma, grad_beta, workspace, stream=None) -> None:
+    """grad_sum, grad_update, grad_gamma and grad_beta may be None; without the last two workspace may be, too."""
+    c = _Call("moe_norm_before_backward", stream)
+    T, H, name, dtype = c.rows(sum)
+    c.done(load_library().moe_norm_before_backward(
+        c.arg(sum, name, T, H), c.arg(gamma, name, H), c.arg(grad_x, name, T, H), c.opt(grad_sum, name, T, H), residual_scale, norm, eps,
+        T, H, dtype, c.arg(grad_residual, name, T, H), c.opt(grad_update, name, T, H), c.opt(grad_gamma, _FLOAT32, H),
+        c.opt(grad_beta, _FLOAT32, H), *c.workspace(workspace), c.stream))
+
+
+def _gate(c: _Call, gate, kind: int, T: int, H: int, name: str) -> Optional[int]:
+    """A gate of this kind; name: type of a channel or full one."""
+    if gate is None:
+        return None
+    if kind == MOE_GATE_CHANNEL:
+        return c.arg(gate, name, H)
+    if kind == MOE_GATE_TOKEN:
+        return c.arg(gate, _FLOAT32, T)
+    return c.arg(gate, name, T, H)
+
+
+def moe_norm_after(residual, y, gamma, beta, gate, gate_kind: int, residual_scale: float, norm: int, eps: float, out,
+                   stream=None) -> None:
+    """out = residual + residual_scale * gate * norm of y; residual and beta may be None, gate is with MOE_GATE_NONE."""
+    c = _Call("moe_norm_after", stream)
+    T, H, name, dtype = c.rows(y)
+    c.done(load_library().moe_norm_after(
+        c.opt(residual, name, T, H), c.arg(y, name, T, H), c.arg(gamma, name, H), c.opt(beta, name, H),
+        _gate(c, gate, gate_kind, T, H, name), gate_kind, residual_scale, norm, eps, T, H, dtype, c.arg(out, name, T, H), c.stream))
+
+
+def moe_norm_after_backward(y, gamma, beta, gate, gate_kind: int, residual_scale: float, grad_out, norm: int, eps: float, grad_y,
+                            grad_gamma, grad_beta, grad_gate, workspace, stream=None) -> None:
+    """grad_gamma, grad_beta and grad_gate may be None; workspace too if nothing is summed over tokens."""
+    c = _Call("moe_norm_after_backward", stream)
+    T, H, name, dtype = c.rows(y)
+    c.done(load_library().moe_norm_after_backward(
+        c.arg(y, name, T, H), c.arg(gamma, name, H), c.opt(beta, name, H), _gate(c, gate, gate_kind, T, H, name), gate_kind,
+        residual_scale, c.arg(grad_out, name, T, H), norm, eps, T, H, dtype, c.arg(grad_y, name, T, H), c.opt(grad_gamma, _FLOAT32, H),
+        c.opt(grad_beta, _FLOAT32, H), _gate(c, grad_gate, gate_kind, T, H, _FLOAT32 if gate_kind == MOE_GATE_CHANNEL else name),
+        *c.workspace(workspace), c.stream))

@@ -1,0 +1,668 @@
+// The norms on either side of the block, with the residual stream: sum and norm in front of it, norm, gate and residual sum
+// behind it, and their gradients.
+//
+// A row stays in registers between its loads and its stores: W wavefronts hold it, NV pieces of 16 bytes a lane, so that every
+// input is read once and every output written once.  Sums over a row are fp32, in a fixed order: lanes by DPP, wavefronts
+// through LDS.  The mean of a "layer" norm is taken off before the squares are summed.
+#include "row_vector.h"
+
+namespace moe {
+
+constexpr int kMinNormColumns = 8, kMaxNormColumns = 16384;
+
+struct NormParams {
+  const char* residual;   // before: the stream; after: the stream or nullptr
+  const char* branch;     // before: what is added to the stream or nullptr; after: the block's output
+  const char* gamma;
+  const char* beta;       // or nullptr
+  const char* gate;
+  char* sum;              // before: the new stream or nullptr
+  char* out;
+  int32_t gate_kind, layer, T;
+  uint32_t row_bytes;
+  float scale, eps, inv_h;
+};
+
+struct NormGradParams {
+  const char* v;          // the rows that were normed
+  const char* g;          // gradient of the outputs
+  const char* gamma;
+  const char* beta;       // after: or nullptr
+  const char* gate;
+  const char* more;       // before: gradient that the stream has by itself, or nullptr
+  char* grad_v;
+  char* grad_other;       // before: scale * grad_v, or nullptr; after: gradient of a full gate, or nullptr
+  float* grad_token_gate; // after: gradient of a token gate, or nullptr
+  float* part_a;          // [groups][H] sums over the rows of a group, or nullptr
+  float* part_b;
+  int32_t gate_kind, layer, T, H, groups;
+  uint32_t row_bytes;
+  float scale, eps, inv_h;
+};
+
+// Sums over the W wavefronts of a row, in every lane of them.  which (0, 1): one of two places in LDS; a wavefront may write the
+// sums of the next row while another still reads the last ones, so sums that follow each other take turns.
+// ragged: the last pieces of a row share bytes, perhaps across two wavefronts, and an output may lie in an input's place: what
+// was requested has to be there before any wavefront goes on to its stores.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int which, bool ragged) {
+  if (ragged) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i++) v[i] = wave_sum(v[i]);
+  if constexpr (W > 1) {
+    __shared__ float part[2][3][W];
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; i++) part[which][i][wave] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      float s = part[which][i][0];
+#pragma unroll
+      for (int w = 1; w < W; w++) s += part[which][i][w];
+      v[i] = s;
+    }
+  }
+}
+
+template <int W> constexpr int threads_of() { return W > 4 ? W * 64 : 256; }
+template <int W> constexpr int rows_of() { return W > 4 ? 1 : 4 / W; }   // rows of a workgroup
+
+template <int DT, int W, int NV, bool AFTER>
+__global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
+  using V = Row<DT>;
+  constexpr int N = V::kVec;
+  const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int t = blockIdx.x * rows_of<W>() + wave / W;
+  if (t >= p.T) return;   // (W > 1: the whole workgroup or nobody)
+  const size_t row = (size_t)t * p.row_bytes;
+  const bool exact = p.row_bytes == W * NV * 1024, ragged = p.row_bytes % 16 != 0;
+  uint32_t at[NV];
+#pragma unroll
+  for (int i = 0; i < NV; i++) at[i] = (uint32_t)((i * W + wave % W) * 64 + lane) * 16;
+  u32x4 rv[NV], bv[NV], gv[NV], hv[NV];
+  if (!AFTER || p.residual != nullptr)
+#pragma unroll
+    for (int i = 0; i < NV; i++) rv[i] = load_piece(p.residual + row, at[i], p.row_bytes);
+  if (AFTER || p.branch != nullptr)
+#pragma unroll
+    for (int i = 0; i < NV; i++) bv[i] = load_piece(p.branch + row, at[i], p.row_bytes);
+  float gate_t = 1.f;
+  if constexpr (AFTER) {
+    if (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL) {
+      const char* gate = p.gate + (p.gate_kind == MOE_GATE_FULL ? row : 0);
+#pragma unroll
+      for (int i = 0; i < NV; i++) hv[i] = load_piece(gate, at[i], p.row_bytes);
+    } else if (p.gate_kind == MOE_GATE_TOKEN) {
+      gate_t = ((const float*)p.gate)[t];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; i++) gv[i] = load_piece(p.gamma, at[i], p.row_bytes);
+  float v[NV][N];
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    if constexpr (AFTER) {
+      V::unpack(bv[i], v[i]);
+    } else {
+      V::unpack(rv[i], v[i]);
+      if (p.branch != nullptr) {
+        float b[N];
+        V::unpack(bv[i], b);
+#pragma unroll
+        for (int c = 0; c < N; c++) v[i][c] = fmaf(p.scale, b[c], v[i][c]);
+      }
+    }
+  }
+  float mean = 0.f, sq[1] = {0.f};
+  if (p.layer) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
+#pragma unroll
+      for (int c = 0; c < N; c++) s[0] += exact || c >= from ? v[i][c] : 0.f;
+    }
+    row_sums<W>(s, 0, false);
+    mean = s[0] * p.inv_h;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+      const float d = v[i][c] - mean;
+      sq[0] = exact || c >= from ? fmaf(d, d, sq[0]) : sq[0];
+    }
+  }
+  row_sums<W>(sq, 1, ragged);
+  const float r = 1.f / sqrtf(fmaf(sq[0], p.inv_h, p.eps));
+  if constexpr (!AFTER)
+    if (p.sum != nullptr)
+#pragma unroll
+      for (int i = 0; i < NV; i++) store_piece(p.sum + row, at[i], p.row_bytes, V::pack(v[i]));
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    float o[N], f[N];
+    V::unpack(gv[i], f);
+#pragma unroll
+    for (int c = 0; c < N; c++) o[c] = (v[i][c] - mean) * r * f[c];
+    if (p.beta != nullptr) {
+      V::unpack(load_piece(p.beta, at[i], p.row_bytes), f);
+#pragma unroll
+      for (int c = 0; c < N; c++) o[c] += f[c];
+    }
+    if constexpr (AFTER) {
+      const float m = p.scale * gate_t;
+      if (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL) {
+        V::unpack(hv[i], f);
+#pragma unroll
+        for (int c = 0; c < N; c++) o[c] *= f[c];
+      }
+#pragma unroll
+      for (int c = 0; c < N; c++) f[c] = 0.f;
+      if (p.residual != nullptr) V::unpack(rv[i], f);
+#pragma unroll
+      for (int c = 0; c < N; c++) o[c] = fmaf(m, o[c], f[c]);
+    }
+    store_piece(p.out + row, at[i], p.row_bytes, V::pack(o));
+  }
+}
+
+// Gradients.  With n the normed row, e the gradient of n and r the reciprocal deviation, the gradient of the row is
+//   r * (e - mean(e) - n * mean(e * n))           (without the mean of e where no mean was taken off).
+// A group of W wavefronts takes rows group, group + groups, ... and keeps, in registers, its columns' sums over them: A of
+// m * n and B of m, m the gradient of gamma * n + beta; they go to part_a and part_b, whose rows k_norm_columns adds up in a
+// fixed order.  A channel gate is a factor of these sums and joins there.  The next row is requested before the present one
+// is summed up (PRE), which the largest rows have no registers for.
+template <int DT, int W, int NV, bool AFTER, bool WITH_B, bool PRE>
+__global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p) {
+  using V = Row<DT>;
+  constexpr int N = V::kVec;
+  const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int group = blockIdx.x * rows_of<W>() + wave / W;
+  if (group >= p.groups) return;   // (W > 1: the whole workgroup or nobody)
+  const bool exact = p.row_bytes == W * NV * 1024, ragged = p.row_bytes % 16 != 0;
+  uint32_t at[NV];
+#pragma unroll
+  for (int i = 0; i < NV; i++) at[i] = (uint32_t)((i * W + wave % W) * 64 + lane) * 16;
+  u32x4 gamma[NV], beta[NV], chan[NV];
+  const bool has_beta = AFTER && p.beta != nullptr, channel = AFTER && p.gate_kind == MOE_GATE_CHANNEL;
+  const bool full = AFTER && p.gate_kind == MOE_GATE_FULL, token = AFTER && p.gate_kind == MOE_GATE_TOKEN;
+#pragma unroll
+  for (int i = 0; i < NV; i++) gamma[i] = load_piece(p.gamma, at[i], p.row_bytes);
+  if constexpr (AFTER) {
+    if (has_beta)
+#pragma unroll
+      for (int i = 0; i < NV; i++) beta[i] = load_piece(p.beta, at[i], p.row_bytes);
+    if (channel)
+#pragma unroll
+      for (int i = 0; i < NV; i++) chan[i] = load_piece(p.gate, at[i], p.row_bytes);
+  }
+  float acc_a[NV][N], acc_b[WITH_B ? NV : 1][N];
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+      acc_a[i][c] = 0.f;
+      if constexpr (WITH_B) acc_b[i][c] = 0.f;
+    }
+  const char* third = AFTER ? (full ? p.gate : nullptr) : p.more;   // the third row that is read, if any
+  u32x4 vv[NV], gg[NV], mm[NV];
+  auto request = [&](int t) {
+    const size_t row = (size_t)t * p.row_bytes;
+#pragma unroll
+    for (int i = 0; i < NV; i++) vv[i] = load_piece(p.v + row, at[i], p.row_bytes);
+#pragma unroll
+    for (int i = 0; i < NV; i++) gg[i] = load_piece(p.g + row, at[i], p.row_bytes);
+    if (third != nullptr)
+#pragma unroll
+      for (int i = 0; i < NV; i++) mm[i] = load_piece(third + row, at[i], p.row_bytes);
+  };
+  int flip = 0;
+  if constexpr (PRE) request(group);
+  for (int t = group; t < p.T; t += p.groups) {
+    const size_t row = (size_t)t * p.row_bytes;
+    if constexpr (!PRE) request(t);
+    float v[NV][N];
+    u32x4 g[NV], m[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      V::unpack(vv[i], v[i]);
+      g[i] = gg[i];
+      m[i] = mm[i];
+    }
+    if constexpr (PRE)
+      if (t + p.groups < p.T) request(t + p.groups);
+    const float gate_t = token ? ((const float*)p.gate)[t] : 1.f;
+    // f: gradient of gamma * n + beta without a token gate or a channel gate; e: of n, without a token gate
+    auto gradients = [&](int i, float (&f)[N], float (&e)[N]) {
+      float x[N];
+      V::unpack(g[i], f);
+      if constexpr (AFTER) {
+#pragma unroll
+        for (int c = 0; c < N; c++) f[c] *= p.scale;
+        if (full) {
+          V::unpack(m[i], x);
+#pragma unroll
+          for (int c = 0; c < N; c++) f[c] *= x[c];
+        }
+      }
+      V::unpack(gamma[i], x);
+#pragma unroll
+      for (int c = 0; c < N; c++) e[c] = f[c] * x[c];
+      if constexpr (AFTER)
+        if (channel) {
+          V::unpack(chan[i], x);
+#pragma unroll
+          for (int c = 0; c < N; c++) e[c] *= x[c];
+        }
+    };
+    float mean = 0.f, mean_e = 0.f;
+    if (p.layer) {
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
+        float f[N], e[N];
+        gradients(i, f, e);
+#pragma unroll
+        for (int c = 0; c < N; c++) {
+          s[0] += exact || c >= from ? v[i][c] : 0.f;
+          s[1] += exact || c >= from ? e[c] : 0.f;
+        }
+      }
+      row_sums<W>(s, flip, false);
+      mean = s[0] * p.inv_h;
+      mean_e = s[1] * p.inv_h;
+    }
+    float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
+      float f[N], e[N];
+      gradients(i, f, e);
+#pragma unroll
+      for (int c = 0; c < N; c++) {
+        const float d = v[i][c] - mean;
+        v[i][c] = d;
+        s[0] = exact || c >= from ? fmaf(d, d, s[0]) : s[0];
+        s[1] = exact || c >= from ? fmaf(e[c], d, s[1]) : s[1];
+      }
+      if (token && has_beta) {
+        float b[N];
+        V::unpack(beta[i], b);
+#pragma unroll
+        for (int c = 0; c < N; c++) s[2] = exact || c >= from ? fmaf(f[c], b[c], s[2]) : s[2];
+      }
+    }
+    row_sums<W>(s, flip, ragged);
+    flip ^= 1;
+    const float r = 1.f / sqrtf(fmaf(s[0], p.inv_h, p.eps));
+    const float en = s[1] * r;   // sum of e * n
+    if (token && p.grad_token_gate != nullptr && lane == 0 && wave % W == 0) p.grad_token_gate[t] = en + s[2];
+    const float mean_en = en * p.inv_h;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float f[N], e[N], o[N];
+      gradients(i, f, e);
+#pragma unroll
+      for (int c = 0; c < N; c++) {
+        const float n = v[i][c] * r;
+        const float fc = f[c] * gate_t;
+        acc_a[i][c] = fmaf(fc, n, acc_a[i][c]);
+        if constexpr (WITH_B) acc_b[i][c] += fc;
+        o[c] = r * gate_t * (e[c] - mean_e - n * mean_en);
+      }
+      if constexpr (!AFTER) {
+        if (p.more != nullptr) {
+          float x[N];
+          V::unpack(m[i], x);
+#pragma unroll
+          for (int c = 0; c < N; c++) o[c] += x[c];
+        }
+        store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
+        if (p.grad_other != nullptr) {
+#pragma unroll
+          for (int c = 0; c < N; c++) o[c] *= p.scale;
+          store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
+        }
+      } else {
+        store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
+        if (full && p.grad_other != nullptr) {
+          float x[N], b[N];
+          V::unpack(gamma[i], x);
+#pragma unroll
+          for (int c = 0; c < N; c++) b[c] = 0.f;
+          if (has_beta) V::unpack(beta[i], b);
+          V::unpack(g[i], f);
+#pragma unroll
+          for (int c = 0; c < N; c++) o[c] = p.scale * f[c] * fmaf(v[i][c] * r, x[c], b[c]);
+          store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
+        }
+      }
+    }
+  }
+  if (p.part_a == nullptr) return;
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    if (at[i] >= p.row_bytes) continue;
+    const size_t col = (size_t)group * p.H + piece_at(at[i], p.row_bytes) / V::kBytes;
+#pragma unroll
+    for (int c = 0; c < N; c++) {
+      p.part_a[col + c] = acc_a[i][c];
+      if constexpr (WITH_B) p.part_b[col + c] = acc_b[i][c];
+    }
+  }
+}
+
+struct NormColumnParams {
+  const float* part_a;
+  const float* part_b;    // or nullptr
+  const char* gamma;
+  const char* beta;       // or nullptr
+  const char* gate;       // a channel gate, or nullptr
+  float* grad_gamma;      // each or nullptr
+  float* grad_beta;
+  float* grad_gate;
+  int32_t groups, H;
+};
+
+// Column sums over the groups: a workgroup takes 32 columns, 32 threads each, which go down the groups in turn and meet in LDS.
+template <int DT>
+__global__ __launch_bounds__(1024) void k_norm_columns(NormColumnParams p) {
+  __shared__ float a[32][33], b[32][33];
+  const int c = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int col = blockIdx.x * 32 + c;
+  float sa = 0.f, sb = 0.f;
+  if (col < p.H) {
+#pragma unroll 8
+    for (int g = part; g < p.groups; g += 32) sa += p.part_a[(size_t)g * p.H + col];
+    if (p.part_b != nullptr)
+#pragma unroll 8
+      for (int g = part; g < p.groups; g += 32) sb += p.part_b[(size_t)g * p.H + col];
+  }
+  a[part][c] = sa;
+  b[part][c] = sb;
+  __syncthreads();
+  if (part != 0 || col >= p.H) return;
+#pragma unroll
+  for (int i = 1; i < 32; i++) {
+    sa += a[i][c];
+    sb += b[i][c];
+  }
+  auto value = [&](const char* v) -> float {
+    if constexpr (DT == MOE_BF16) return __uint_as_float((uint32_t)((const uint16_t*)v)[col] << 16);
+    else if constexpr (DT == MOE_FP16) return (float)((const _Float16*)v)[col];
+    else return ((const float*)v)[col];
+  };
+  const float gate = p.gate != nullptr ? value(p.gate) : 1.f;
+  if (p.grad_gamma != nullptr) p.grad_gamma[col] = sa * gate;
+  if (p.grad_beta != nullptr) p.grad_beta[col] = sb * gate;
+  if (p.grad_gate != nullptr) p.grad_gate[col] = value(p.gamma) * sa + (p.beta != nullptr ? value(p.beta) * sb : 0.f);
+}
+
+namespace {
+
+constexpr int kGroups1 = 2048, kGroups4 = 512, kGroups8 = 256;   // groups of rows, with 1, 4, and 8 or 16 wavefronts a row
+
+// Wavefronts that hold a row, from its pieces of 16 bytes, and pieces a lane.
+int waves_of(uint32_t pieces) { return pieces <= 256 ? 1 : pieces <= 512 ? 4 : pieces <= 1024 ? 8 : 16; }
+int groups_of(int T, uint32_t pieces) {
+  const int waves = waves_of(pieces), most = waves == 1 ? kGroups1 : waves == 4 ? kGroups4 : kGroups8;
+  return T < most ? T : most;
+}
+uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
+
+template <int DT, bool AFTER, int W, int NV>
+hipError_t norm_as(const NormParams& p, hipStream_t st) {
+  hipLaunchKernelGGL((k_norm<DT, W, NV, AFTER>), dim3((unsigned)((p.T + rows_of<W>() - 1) / rows_of<W>())), dim3(threads_of<W>()), 0, st, p);
+  return hipGetLastError();
+}
+template <int DT, bool AFTER>
+hipError_t norm_type(const NormParams& p, hipStream_t st) {
+  const uint32_t n = pieces_of(p.row_bytes);
+  if (n <= 64) return norm_as<DT, AFTER, 1, 1>(p, st);
+  if (n <= 128) return norm_as<DT, AFTER, 1, 2>(p, st);
+  if (n <= 256) return norm_as<DT, AFTER, 1, 4>(p, st);
+  if (n <= 512) return norm_as<DT, AFTER, 4, 2>(p, st);
+  if (n <= 1024) return norm_as<DT, AFTER, 8, 2>(p, st);
+  if (n <= 2048) return norm_as<DT, AFTER, 16, 2>(p, st);
+  if constexpr (DT == MOE_FP32) return norm_as<DT, AFTER, 16, 4>(p, st);
+  return hipErrorInvalidValue;   // (no row of two-byte elements is that long)
+}
+template <bool AFTER>
+hipError_t launch_norm(int dtype, const NormParams& p, hipStream_t st) {
+  switch (dtype) {
+    case MOE_BF16: return norm_type<MOE_BF16, AFTER>(p, st);
+    case MOE_FP16: return norm_type<MOE_FP16, AFTER>(p, st);
+    default: return norm_type<MOE_FP32, AFTER>(p, st);
+  }
+}
+
+template <int DT, bool AFTER, bool WITH_B, int W, int NV>
+hipError_t norm_grad_as(const NormGradParams& p, hipStream_t st) {
+  hipLaunchKernelGGL((k_norm_grad<DT, W, NV, AFTER, WITH_B, (W <= 8)>), dim3((unsigned)((p.groups + rows_of<W>() - 1) / rows_of<W>())),
+                     dim3(threads_of<W>()), 0, st, p);
+  return hipGetLastError();
+}
+template <int DT, bool AFTER, bool WITH_B>
+hipError_t norm_grad_b(const NormGradParams& p, hipStream_t st) {
+  const uint32_t n = pieces_of(p.row_bytes);
+  if (n <= 64) return norm_grad_as<DT, AFTER, WITH_B, 1, 1>(p, st);
+  if (n <= 128) return norm_grad_as<DT, AFTER, WITH_B, 1, 2>(p, st);
+  if (n <= 256) return norm_grad_as<DT, AFTER, WITH_B, 1, 4>(p, st);
+  if (n <= 512) return norm_grad_as<DT, AFTER, WITH_B, 4, 2>(p, st);
+  if (n <= 1024) return norm_grad_as<DT, AFTER, WITH_B, 8, 2>(p, st);
+  if (n <= 2048) return norm_grad_as<DT, AFTER, WITH_B, 16, 2>(p, st);
+  if constexpr (DT == MOE_FP32) return norm_grad_as<DT, AFTER, WITH_B, 16, 4>(p, st);
+  return hipErrorInvalidValue;   // (no row of two-byte elements is that long)
+}
+template <int DT, bool AFTER>
+hipError_t norm_grad_type(const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
+  if (p.groups > 0) {
+    const hipError_t e = p.part_b != nullptr ? norm_grad_b<DT, AFTER, true>(p, st) : norm_grad_b<DT, AFTER, false>(p, st);
+    if (e != hipSuccess) return e;
+  }
+  if (!cp.grad_gamma && !cp.grad_beta && !cp.grad_gate) return hipSuccess;
+  hipLaunchKernelGGL(k_norm_columns<DT>, dim3((unsigned)((cp.H + 31) / 32)), dim3(1024), 0, st, cp);
+  return hipGetLastError();
+}
+template <bool AFTER>
+hipError_t launch_norm_grad(int dtype, const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
+  switch (dtype) {
+    case MOE_BF16: return norm_grad_type<MOE_BF16, AFTER>(p, cp, st);
+    case MOE_FP16: return norm_grad_type<MOE_FP16, AFTER>(p, cp, st);
+    default: return norm_grad_type<MOE_FP32, AFTER>(p, cp, st);
+  }
+}
+
+int norm_shape(int32_t T, int32_t H) {
+  if (T < 0 || H <= 0) return MOE_ERR_INVALID_ARG;
+  if (H < kMinNormColumns || H > kMaxNormColumns || T >= (1 << 24)) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+int norm_call(int32_t T, int32_t H, int32_t dtype, int32_t norm, float eps, float scale) {
+  if (element_bytes(dtype) == 0 || (norm != MOE_NORM_RMS && norm != MOE_NORM_LAYER)) return MOE_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || !(eps < 1e30f) || !(scale > -1e30f && scale < 1e30f)) return MOE_ERR_INVALID_ARG;
+  const int rc = norm_shape(T, H);
+  if (rc != MOE_OK) return rc;
+  return (int64_t)T * H * element_bytes(dtype) < (1ll << 36) ? MOE_OK : MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
+}
+bool gate_ok(const void* gate, int32_t gate_kind, bool rows) {
+  if (gate_kind < MOE_GATE_NONE || gate_kind > MOE_GATE_FULL) return false;
+  if (gate_kind == MOE_GATE_NONE) return gate == nullptr;
+  return (gate != nullptr || (!rows && gate_kind != MOE_GATE_CHANNEL)) && aligned16(gate);
+}
+// An output may lie in the place of an input of the same rows, not across it.
+bool apart(const void* out, const void* in, size_t bytes) { return !out || !in || out == in || !overlap(out, bytes, in, bytes); }
+
+int status_of(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
+
+}  // namespace
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+int moe_norm_before(const void* residual, const void* update, float residual_scale, const void* gamma, const void* beta,
+                    int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void* sum, void* x, void* hip_stream) {
+  const int rc = norm_call(T, H, dtype, norm, eps, residual_scale);
+  if (rc != MOE_OK) return rc;
+  if (T == 0) return MOE_OK;
+  if (!residual || !gamma || !x) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(residual) || !aligned16(update) || !aligned16(gamma) || !aligned16(beta) || !aligned16(sum) || !aligned16(x))
+    return MOE_ERR_INVALID_ARG;
+  const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
+  if (!apart(sum, residual, bytes) || !apart(sum, update, bytes) || !apart(x, residual, bytes) || !apart(x, update, bytes))
+    return MOE_ERR_INVALID_ARG;
+  if (sum && overlap(sum, bytes, x, bytes)) return MOE_ERR_INVALID_ARG;
+  NormParams p = {};
+  p.residual = (const char*)residual;
+  p.branch = (const char*)update;
+  p.gamma = (const char*)gamma;
+  p.beta = (const char*)beta;
+  p.sum = (char*)sum;
+  p.out = (char*)x;
+  p.layer = norm == MOE_NORM_LAYER;
+  p.T = T;
+  p.row_bytes = (uint32_t)row_bytes;
+  p.scale = residual_scale;
+  p.eps = eps;
+  p.inv_h = 1.0f / (float)H;
+  return status_of(launch_norm<false>(dtype, p, (hipStream_t)hip_stream));
+}
+
+int moe_norm_after(const void* residual, const void* y, const void* gamma, const void* beta, const void* gate, int32_t gate_kind,
+                   float residual_scale, int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void* out, void* hip_stream) {
+  const int rc = norm_call(T, H, dtype, norm, eps, residual_scale);
+  if (rc != MOE_OK) return rc;
+  if (!gate_ok(gate, gate_kind, T > 0)) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return MOE_OK;
+  if (!y || !gamma || !out) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(residual) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
+  const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
+  if (!apart(out, residual, bytes) || !apart(out, y, bytes) || (gate_kind == MOE_GATE_FULL && !apart(out, gate, bytes))) return MOE_ERR_INVALID_ARG;
+  NormParams p = {};
+  p.residual = (const char*)residual;
+  p.branch = (const char*)y;
+  p.gamma = (const char*)gamma;
+  p.beta = (const char*)beta;
+  p.gate = (const char*)gate;
+  p.gate_kind = gate_kind;
+  p.out = (char*)out;
+  p.layer = norm == MOE_NORM_LAYER;
+  p.T = T;
+  p.row_bytes = (uint32_t)row_bytes;
+  p.scale = residual_scale;
+  p.eps = eps;
+  p.inv_h = 1.0f / (float)H;
+  return status_of(launch_norm<true>(dtype, p, (hipStream_t)hip_stream));
+}
+
+size_t moe_norm_workspace_bytes(int32_t T, int32_t H) {
+  if (norm_shape(T, H) != MOE_OK) return 0;
+  const int groups2 = groups_of(T, pieces_of((uint32_t)H * 2)), groups4 = groups_of(T, pieces_of((uint32_t)H * 4));
+  const size_t groups = groups2 > groups4 ? groups2 : groups4;
+  return 2 * (groups > 0 ? groups : 1) * (size_t)H * 4;
+}
+
+int moe_norm_before_backward(const void* sum, const void* gamma, const void* grad_x, const void* grad_sum, float residual_scale,
+                             int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void* grad_residual, void* grad_update,
+                             float* grad_gamma, float* grad_beta, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = norm_call(T, H, dtype, norm, eps, residual_scale);
+  if (rc != MOE_OK) return rc;
+  const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
+  const bool columns = grad_gamma || grad_beta;
+  if (!gamma || (T > 0 && (!sum || !grad_x || !grad_residual)) || (columns && !workspace)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(sum) || !aligned16(gamma) || !aligned16(grad_x) || !aligned16(grad_sum) || !aligned16(grad_residual) ||
+      !aligned16(grad_update) || !aligned16(grad_gamma) || !aligned16(grad_beta) || !aligned16(workspace))
+    return MOE_ERR_INVALID_ARG;
+  if (columns && workspace_bytes < moe_norm_workspace_bytes(T, H)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  for (void* out : {grad_residual, grad_update})
+    if (!apart(out, sum, bytes) || !apart(out, grad_x, bytes) || !apart(out, grad_sum, bytes)) return MOE_ERR_INVALID_ARG;
+  if (grad_update && T > 0 && overlap(grad_update, bytes, grad_residual, bytes)) return MOE_ERR_INVALID_ARG;
+  NormGradParams p = {};
+  p.v = (const char*)sum;
+  p.g = (const char*)grad_x;
+  p.gamma = (const char*)gamma;
+  p.more = (const char*)grad_sum;
+  p.grad_v = (char*)grad_residual;
+  p.grad_other = (char*)grad_update;
+  p.layer = norm == MOE_NORM_LAYER;
+  p.T = T;
+  p.H = H;
+  p.row_bytes = (uint32_t)row_bytes;
+  p.groups = groups_of(T, pieces_of(p.row_bytes));
+  p.part_a = columns ? (float*)workspace : nullptr;
+  p.part_b = grad_beta ? p.part_a + (size_t)p.groups * H : nullptr;
+  p.scale = residual_scale;
+  p.eps = eps;
+  p.inv_h = 1.0f / (float)H;
+  NormColumnParams cp = {};
+  cp.part_a = p.part_a;
+  cp.part_b = p.part_b;
+  cp.gamma = p.gamma;
+  cp.grad_gamma = grad_gamma;
+  cp.grad_beta = grad_beta;
+  cp.groups = p.groups;
+  cp.H = H;
+  return status_of(launch_norm_grad<false>(dtype, p, cp, (hipStream_t)hip_stream));
+}
+
+int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, const void* gate, int32_t gate_kind,
+                            float residual_scale, const void* grad_out, int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype,
+                            void* grad_y, float* grad_gamma, float* grad_beta, void* grad_gate, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  const int rc = norm_call(T, H, dtype, norm, eps, residual_scale);
+  if (rc != MOE_OK) return rc;
+  if (!gate_ok(gate, gate_kind, T > 0) || (gate_kind == MOE_GATE_NONE && grad_gate)) return MOE_ERR_INVALID_ARG;
+  const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
+  const bool channel = gate_kind == MOE_GATE_CHANNEL, columns = grad_gamma || grad_beta || (channel && grad_gate);
+  if (!gamma || (T > 0 && (!y || !grad_out || !grad_y)) || (columns && !workspace)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(grad_out) || !aligned16(grad_y) || !aligned16(grad_gamma) ||
+      !aligned16(grad_beta) || !aligned16(grad_gate) || !aligned16(workspace))
+    return MOE_ERR_INVALID_ARG;
+  if (columns && workspace_bytes < moe_norm_workspace_bytes(T, H)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  const bool full = gate_kind == MOE_GATE_FULL;
+  for (void* out : {grad_y, full ? grad_gate : nullptr})
+    if (!apart(out, y, bytes) || !apart(out, grad_out, bytes) || (full && !apart(out, gate, bytes))) return MOE_ERR_INVALID_ARG;
+  if (full && grad_gate && T > 0 && overlap(grad_gate, bytes, grad_y, bytes)) return MOE_ERR_INVALID_ARG;
+  NormGradParams p = {};
+  p.v = (const char*)y;
+  p.g = (const char*)grad_out;
+  p.gamma = (const char*)gamma;
+  p.beta = (const char*)beta;
+  p.gate = (const char*)gate;
+  p.gate_kind = gate_kind;
+  p.grad_v = (char*)grad_y;
+  p.grad_other = full ? (char*)grad_gate : nullptr;
+  p.grad_token_gate = gate_kind == MOE_GATE_TOKEN ? (float*)grad_gate : nullptr;
+  p.layer = norm == MOE_NORM_LAYER;
+  p.T = T;
+  p.H = H;
+  p.row_bytes = (uint32_t)row_bytes;
+  p.groups = groups_of(T, pieces_of(p.row_bytes));
+  p.part_a = columns ? (float*)workspace : nullptr;
+  p.part_b = grad_beta || (channel && grad_gate && beta) ? p.part_a + (size_t)p.groups * H : nullptr;
+  p.scale = residual_scale;
+  p.eps = eps;
+  p.inv_h = 1.0f / (float)H;
+  NormColumnParams cp = {};
+  cp.part_a = p.part_a;
+  cp.part_b = p.part_b;
+  cp.gamma = p.gamma;
+  cp.beta = p.beta;
+  cp.gate = channel ? p.gate : nullptr;
+  cp.grad_gamma = grad_gamma;
+  cp.grad_beta = grad_beta;
+  cp.grad_gate = channel ? (float*)grad_gate : nullptr;
+  cp.groups = p.groups;
+  cp.H = H;
+  return status_of(launch_norm_grad<true>(dtype, p, cp, (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

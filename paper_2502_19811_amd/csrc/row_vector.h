@@ -1,0 +1,105 @@
+// Rows of bf16, fp16 or fp32 in 16-byte pieces, for the operators around the experts.
+//
+// A row of H >= 8 elements starts at a multiple of its element's size only (H may be odd), so a piece is loaded and stored with
+// the alignment of its element: global memory instructions of gfx950 take any.  The last piece of a row that is not a multiple
+// of 16 bytes lies over the one before it, which needs no code of its own for what is left.
+#pragma once
+#include "moe_device.h"
+
+namespace moe {
+
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <int DT> struct Row;
+template <> struct Row<MOE_BF16> {
+  static constexpr int kBytes = 2, kVec = 8;
+  static __device__ __forceinline__ void unpack(const u32x4& v, float (&f)[8]) {
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      f[2 * c] = __uint_as_float(v[c] << 16);
+      f[2 * c + 1] = __uint_as_float(v[c] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
+    u32x4 v;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const bf16x2 pr = {(__bf16)f[2 * c], (__bf16)f[2 * c + 1]};
+      v[c] = __builtin_bit_cast(uint32_t, pr);
+    }
+    return v;
+  }
+};
+template <> struct Row<MOE_FP16> {
+  static constexpr int kBytes = 2, kVec = 8;
+  typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+  static __device__ __forceinline__ void unpack(const u32x4& v, float (&f)[8]) {
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const f16x2 pr = __builtin_bit_cast(f16x2, (uint32_t)v[c]);
+      f[2 * c] = (float)pr[0];
+      f[2 * c + 1] = (float)pr[1];
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
+    u32x4 v;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const f16x2 pr = {(_Float16)f[2 * c], (_Float16)f[2 * c + 1]};
+      v[c] = __builtin_bit_cast(uint32_t, pr);
+    }
+    return v;
+  }
+};
+template <> struct Row<MOE_FP32> {
+  static constexpr int kBytes = 4, kVec = 4;
+  static __device__ __forceinline__ void unpack(const u32x4& v, float (&f)[4]) {
+#pragma unroll
+    for (int c = 0; c < 4; c++) f[c] = __uint_as_float(v[c]);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[4]) {
+    u32x4 v;
+#pragma unroll
+    for (int c = 0; c < 4; c++) v[c] = __float_as_uint(f[c]);
+    return v;
+  }
+};
+
+// A thread's piece of a row is meant to start at byte `start`; it is taken from where a whole piece still fits.  Elements that
+// two pieces then hold are computed twice, alike, and stored twice; sums leave them out of the later one: counted() tells.
+__device__ __forceinline__ uint32_t piece_at(uint32_t start, uint32_t row_bytes) { return min(start, row_bytes - 16); }
+__device__ __forceinline__ u32x4 load_piece(const char* row, uint32_t start, uint32_t row_bytes) {
+  return *(const u32x4_any*)(row + piece_at(start, row_bytes));
+}
+__device__ __forceinline__ void store_piece(char* row, uint32_t start, uint32_t row_bytes, const u32x4& v) {
+  if (start < row_bytes) *(u32x4_any*)(row + piece_at(start, row_bytes)) = v;
+}
+// First element of the piece that counts in a sum over the row (0: all of them; kVec and more: none).
+template <int UNIT>
+__device__ __forceinline__ int counted(uint32_t start, uint32_t row_bytes) { return (int)((start - piece_at(start, row_bytes)) / UNIT); }
+
+// Sum over the wavefront in a fixed order, in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+  auto step = [&](auto ctrl, auto rows) {   // lanes the control does not reach add 0
+    v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+  };
+  step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1, 2, 4, 8: the last lane of
+  step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});   // every 16 has their sum
+  step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15, 31: the last lane of all
+  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+
+// Bytes of an element, 0: no such type.
+inline int element_bytes(int dtype) { return dtype == MOE_BF16 || dtype == MOE_FP16 ? 2 : dtype == MOE_FP32 ? 4 : 0; }
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Whether two buffers share bytes.
+inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
+}  // namespace moe

@@ -1,0 +1,634 @@
+// Tokens to rows in expert order and back, as operators of their own: row order from the experts of the pairs, dispatch of the
+// tokens' rows, combine with the weights, their gradients, and the gate's gradient.
+//
+// With pairs q = t*k + j and e(q) the expert of pair q, the row of q is the number of pairs of lower experts plus the number of
+// its own expert's pairs before it; pairs without an expert have no row.  All of it is data movement: a row is read once and
+// written once, sums over a token's k rows and over a row's columns are fp32 in a fixed order.
+#include "row_vector.h"
+
+namespace moe {
+
+constexpr int kSortChunk = 1024;        // pairs of a workgroup
+constexpr int kSortSmall = 4096;        // pairs up to which one workgroup does it all
+constexpr int kBuckets = kMaxExperts + 1;   // the last one, number E, takes the pairs without an expert
+constexpr int kMaxGateTopK = 64;
+constexpr int kMinRowColumns = 8, kMaxRowColumns = 65536;
+
+__device__ __forceinline__ int bucket_of(const int32_t* ids, int q, int E) {
+  const int e = ids[q];
+  return (unsigned)e < (unsigned)E ? e : E;
+}
+
+// Lanes of the wavefront with the same bucket (up to 9 bits) as this one, among the valid ones.
+__device__ __forceinline__ uint64_t same_bucket(int e, bool valid) {
+  uint64_t same = __ballot(valid);
+#pragma unroll
+  for (int bit = 0; bit < 9; bit++) {
+    const uint64_t b = __ballot((e >> bit) & 1);
+    same &= ((e >> bit) & 1) ? b : ~b;
+  }
+  return same;
+}
+
+// Exclusive prefix sum over kBuckets values in LDS, by the first wavefront.
+__device__ __forceinline__ void scan_buckets(const int32_t* count, int32_t* first) {
+  constexpr int kEach = (kBuckets + 63) / 64;
+  if (threadIdx.x >= 64) return;
+  const int lane = threadIdx.x;
+  int v[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; i++) {
+    const int e = lane * kEach + i;
+    v[i] = e < kBuckets ? count[e] : 0;
+    sum += v[i];
+  }
+  int incl = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  int at = incl - sum;
+#pragma unroll
+  for (int i = 0; i < kEach; i++) {
+    const int e = lane * kEach + i;
+    if (e < kBuckets) first[e] = at;
+    at += v[i];
+  }
+}
+
+// One workgroup for up to RUNS * 64 pairs: runs of 64 pairs, ranks inside a run by ballots, then prefix sums over the runs.
+template <int RUNS>
+__global__ __launch_bounds__(1024) void k_sort_small(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ offsets,
+                                                     int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
+  constexpr int kEach = (RUNS + 15) / 16;
+  __shared__ uint16_t run_cnt[RUNS][kBuckets];
+  __shared__ int32_t count[kBuckets], first[kBuckets];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int key[kEach], rank[kEach];
+#pragma unroll
+  for (int s = 0; s < kEach; s++) {
+    const int q = (wave * kEach + s) * 64 + lane;
+    key[s] = q < R ? bucket_of(ids, q, E) : -1;
+  }
+  for (int i = threadIdx.x; i < RUNS * kBuckets; i += blockDim.x) (&run_cnt[0][0])[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < kEach; s++) {
+    const int run = wave * kEach + s;
+    const uint64_t same = same_bucket(key[s], key[s] >= 0), below = same & ((1ull << lane) - 1ull);
+    rank[s] = __popcll(below);
+    if (key[s] >= 0 && below == 0) run_cnt[run][key[s]] = (uint16_t)__popcll(same);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < kBuckets; e += blockDim.x) {
+    int acc = 0;
+#pragma unroll
+    for (int r = 0; r < RUNS; r++) {
+      const int c = run_cnt[r][e];
+      run_cnt[r][e] = (uint16_t)acc;
+      acc += c;
+    }
+    count[e] = acc;
+  }
+  __syncthreads();
+  scan_buckets(count, first);
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < kEach; s++) {
+    const int run = wave * kEach + s, q = run * 64 + lane, e = key[s];
+    if (e < 0) continue;
+    const int pos = first[e] + run_cnt[run][e] + rank[s];
+    perm[pos] = e < E ? q : -1;
+    inv[q] = e < E ? pos : -1;
+  }
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) offsets[e] = first[e];
+}
+
+// Pairs of each bucket in each chunk.
+__global__ __launch_bounds__(1024) void k_sort_hist(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ hist) {
+  __shared__ int32_t count[kBuckets];
+  for (int e = threadIdx.x; e <= E; e += 1024) count[e] = 0;
+  __syncthreads();
+  const int q = blockIdx.x * kSortChunk + threadIdx.x;
+  if (q < R) atomicAdd(&count[bucket_of(ids, q, E)], 1);
+  __syncthreads();
+  for (int e = threadIdx.x; e <= E; e += 1024) hist[(size_t)blockIdx.x * (E + 1) + e] = count[e];
+}
+
+// Many chunks: one workgroup per bucket turns its counts into prefix sums over the chunks, and leaves the total.
+__global__ __launch_bounds__(1024) void k_sort_scan(int32_t* __restrict__ hist, int n_chunks, int E, int32_t* __restrict__ total) {
+  __shared__ int32_t wave_sum_[16];
+  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int at = 0;
+  for (int b0 = 0; b0 < n_chunks; b0 += 1024) {
+    const int b = b0 + threadIdx.x;
+    const int v = b < n_chunks ? hist[(size_t)b * (E + 1) + e] : 0;
+    int incl = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 63) wave_sum_[wave] = incl;
+    __syncthreads();
+    int before = at, sum = 0;
+#pragma unroll
+    for (int w = 0; w < 16; w++) {
+      const int c = wave_sum_[w];
+      if (w < wave) before += c;
+      sum += c;
+    }
+    if (b < n_chunks) hist[(size_t)b * (E + 1) + e] = before + incl - v;
+    at += sum;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) total[e] = at;
+}
+
+// Stable scatter of a chunk.  total == nullptr: hist holds counts, and the workgroup sums those of the other chunks itself
+// (a thread per bucket and part of the chunks); otherwise hist holds the prefix sums.
+__global__ __launch_bounds__(1024) void k_sort_scatter(const int32_t* __restrict__ ids, int R, int E, const int32_t* __restrict__ hist,
+                                                       int n_chunks, const int32_t* __restrict__ total, int32_t* __restrict__ offsets,
+                                                       int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
+  constexpr int kRuns = kSortChunk / 64;
+  __shared__ int32_t run_cnt[kRuns][kBuckets];
+  __shared__ int32_t count[kBuckets], first[kBuckets], before[kBuckets];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = E + 1;
+  const int q = blockIdx.x * kSortChunk + threadIdx.x;
+  const int e = q < R ? bucket_of(ids, q, E) : -1;
+  for (int i = threadIdx.x; i < kRuns * kBuckets; i += 1024) (&run_cnt[0][0])[i] = 0;
+  for (int i = threadIdx.x; i < kBuckets; i += 1024) {
+    count[i] = total != nullptr && i < n ? total[i] : 0;
+    before[i] = total != nullptr && i < n ? hist[(size_t)blockIdx.x * n + i] : 0;
+  }
+  __syncthreads();
+  if (total == nullptr) {
+    const int parts = n <= 1024 / 16 ? 16 : n <= 1024 / 8 ? 8 : 3;
+    const int b = threadIdx.x % n, part = threadIdx.x / n;
+    if (part < parts) {
+      int all = 0, mine = 0;
+#pragma unroll 8
+      for (int c = part; c < n_chunks; c += parts) {
+        const int v = hist[(size_t)c * n + b];
+        all += v;
+        mine += c < (int)blockIdx.x ? v : 0;
+      }
+      atomicAdd(&count[b], all);   // (whole numbers: the order does not show)
+      atomicAdd(&before[b], mine);
+    }
+  }
+  const uint64_t same = same_bucket(e, e >= 0), below = same & ((1ull << lane) - 1ull);
+  const int rank = __popcll(below);
+  if (e >= 0 && below == 0) run_cnt[wave][e] = __popcll(same);
+  __syncthreads();
+  scan_buckets(count, first);
+  for (int i = threadIdx.x - 64; i >= 0 && i < n; i += 1024 - 64) {   // (the first wavefront is scanning)
+    int acc = before[i];
+#pragma unroll
+    for (int r = 0; r < kRuns; r++) {
+      const int c = run_cnt[r][i];
+      run_cnt[r][i] = acc;
+      acc += c;
+    }
+  }
+  __syncthreads();
+  if (e >= 0) {
+    const int pos = first[e] + run_cnt[wave][e] + rank;
+    perm[pos] = e < E ? q : -1;
+    inv[q] = e < E ? pos : -1;
+  }
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i <= E; i += 1024) offsets[i] = first[i];
+}
+
+__global__ void k_sort_none(int E, int32_t* __restrict__ offsets) {
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) offsets[e] = 0;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows.  LP lanes work on a token (64, or fewer where a row has few pieces of 16 bytes); with 64 everything about the
+// token is the same in every lane and stays in scalar registers.
+// ---------------------------------------------------------------------------------------------
+template <int LP>
+struct Unit {
+  int wave, t, lane, span;
+  __device__ __forceinline__ Unit(int spans) {
+    wave = uniform((int)(threadIdx.x >> 6));
+    const int u = blockIdx.x * 4 + wave;
+    lane = threadIdx.x & (LP - 1);
+    if constexpr (LP == 64) {
+      t = u / spans;
+      span = u - t * spans;
+    } else {
+      t = u * (64 / LP) + (int)((threadIdx.x & 63) / LP);
+      span = 0;
+    }
+  }
+};
+
+// rows[inv[t][j]] = x[t]: a token's row is read once and written k times.
+template <int LP, int NV>
+__global__ __launch_bounds__(256) void k_dispatch(const char* x, const int32_t* __restrict__ inv, char* rows, int T, int k, int R,
+                                                  uint32_t row_bytes, int spans) {
+  constexpr int kGroup = 4;
+  const Unit<LP> at(spans);
+  if (at.t >= T) return;
+  const char* src = x + (size_t)at.t * row_bytes;
+  const uint32_t start = (uint32_t)at.span * (64 * 16 * NV) + at.lane * 16;
+  u32x4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; i++) v[i] = load_piece(src, start + i * (LP * 16), row_bytes);
+  for (int j0 = 0; j0 < k; j0 += kGroup) {
+    int pos[kGroup];
+#pragma unroll
+    for (int j = 0; j < kGroup; j++) pos[j] = j0 + j < k ? inv[(size_t)at.t * k + j0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < kGroup; j++) {
+      if ((unsigned)pos[j] >= (unsigned)R) continue;   // no row
+      char* dst = rows + (size_t)pos[j] * row_bytes;
+#pragma unroll
+      for (int i = 0; i < NV; i++) store_piece(dst, start + i * (LP * 16), row_bytes, v[i]);
+    }
+  }
+}
+
+// out[t] = sum_j w[t][j] * rows[inv[t][j]] in the order of j, without weights the plain sum.  K > 0: up to K slots, the rows of
+// all requested before the first is used; K == 0: any number, slot after slot.
+template <int DT, int K, int LP, int NV>
+__global__ __launch_bounds__(256) void k_combine_rows(const char* rows, const int32_t* __restrict__ inv, const float* __restrict__ w,
+                                                      char* out, int T, int k, int R, uint32_t row_bytes, int spans) {
+  using V = Row<DT>;
+  constexpr int N = V::kVec, KK = K > 0 ? K : 1;
+  const Unit<LP> at(spans);
+  if (at.t >= T) return;
+  const uint32_t start = (uint32_t)at.span * (64 * 16 * NV) + at.lane * 16;
+  float acc[NV][N];
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int c = 0; c < N; c++) acc[i][c] = 0.f;
+  for (int j0 = 0; j0 < (K > 0 ? 1 : k); j0++) {
+    int pos[KK];
+    float wj[KK];
+    u32x4 v[KK][NV];
+#pragma unroll
+    for (int j = 0; j < KK; j++) {
+      const bool there = K == 0 || j < k;
+      pos[j] = there ? inv[(size_t)at.t * k + j0 + j] : -1;
+      wj[j] = there && w != nullptr ? w[(size_t)at.t * k + j0 + j] : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < KK; j++)
+      if ((unsigned)pos[j] < (unsigned)R)
+#pragma unroll
+        for (int i = 0; i < NV; i++) v[j][i] = load_piece(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
+#pragma unroll
+    for (int j = 0; j < KK; j++)
+      if ((unsigned)pos[j] < (unsigned)R)
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+          float f[N];
+          V::unpack(v[j][i], f);
+#pragma unroll
+          for (int c = 0; c < N; c++) acc[i][c] = fmaf(wj[j], f[c], acc[i][c]);
+        }
+  }
+  char* dst = out + (size_t)at.t * row_bytes;
+#pragma unroll
+  for (int i = 0; i < NV; i++) store_piece(dst, start + i * (LP * 16), row_bytes, V::pack(acc[i]));
+}
+
+// grad_rows[inv[t][j]] = w[t][j] * g[t], grad_w[t][j] = <g[t], rows[inv[t][j]]>, 0 for a slot without a row.  A token belongs to
+// WAVES wavefronts of one workgroup (LP == 64), which take its pieces in turn and add their sums up in LDS, or to LP lanes.
+// rows == nullptr: no grad_w.
+template <int DT, int K, int LP, int NV, int WAVES>
+__global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char* rows, const int32_t* __restrict__ inv,
+                                                      const float* __restrict__ w, char* grad_rows, float* __restrict__ grad_w, int T,
+                                                      int k, int R, uint32_t row_bytes) {
+  using V = Row<DT>;
+  constexpr int N = V::kVec, KK = K > 0 ? K : 1;
+  constexpr uint32_t kStep = WAVES * LP * 16 * NV;
+  __shared__ float part[WAVES > 1 ? KK : 1][4];
+  Unit<LP> at(1);
+  if constexpr (WAVES > 1) at.t = blockIdx.x;
+  if (at.t >= T) return;   // (WAVES > 1: the whole workgroup or nobody)
+  const char* src = g + (size_t)at.t * row_bytes;
+  const bool exact = row_bytes % kStep == 0;
+  for (int j0 = 0; j0 < k; j0 += K > 0 ? k : 1) {
+    int pos[KK];
+    float wj[KK], dot[KK];
+#pragma unroll
+    for (int j = 0; j < KK; j++) {
+      const bool there = K == 0 || j < k;
+      pos[j] = there ? inv[(size_t)at.t * k + j0 + j] : -1;
+      wj[j] = there && w != nullptr ? w[(size_t)at.t * k + j0 + j] : 1.f;
+      dot[j] = 0.f;
+    }
+    for (uint32_t base = WAVES > 1 ? at.wave * (64 * 16 * NV) : 0; base < row_bytes; base += kStep) {
+      const uint32_t start = base + at.lane * 16;
+      u32x4 gv[NV], rv[KK][NV];
+#pragma unroll
+      for (int i = 0; i < NV; i++) gv[i] = load_piece(src, start + i * (LP * 16), row_bytes);
+      if (rows != nullptr) {
+#pragma unroll
+        for (int j = 0; j < KK; j++)
+          if ((unsigned)pos[j] < (unsigned)R)
+#pragma unroll
+            for (int i = 0; i < NV; i++) rv[j][i] = load_piece(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        const int from = exact ? 0 : counted<V::kBytes>(start + i * (LP * 16), row_bytes);
+        float gf[N];
+        V::unpack(gv[i], gf);
+#pragma unroll
+        for (int j = 0; j < KK; j++) {
+          if ((unsigned)pos[j] >= (unsigned)R) continue;
+          if (rows != nullptr) {
+            float rf[N];
+            V::unpack(rv[j][i], rf);
+            if (exact) {
+#pragma unroll
+              for (int c = 0; c < N; c++) dot[j] = fmaf(gf[c], rf[c], dot[j]);
+            } else {
+#pragma unroll
+              for (int c = 0; c < N; c++) dot[j] = c >= from ? fmaf(gf[c], rf[c], dot[j]) : dot[j];
+            }
+          }
+          float o[N];
+#pragma unroll
+          for (int c = 0; c < N; c++) o[c] = wj[j] * gf[c];
+          store_piece(grad_rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes, V::pack(o));
+        }
+      }
+    }
+    if (rows == nullptr) continue;
+#pragma unroll
+    for (int j = 0; j < KK; j++) {
+      if constexpr (LP == 64) {
+        dot[j] = wave_sum(dot[j]);
+      } else {
+#pragma unroll
+        for (int off = LP / 2; off >= 1; off >>= 1) dot[j] += __shfl_xor(dot[j], off);
+      }
+      if constexpr (WAVES == 1) {
+        if (at.lane == 0 && (K == 0 || j < k)) grad_w[(size_t)at.t * k + j0 + j] = dot[j];
+      } else {
+        if (at.lane == 0) part[j][at.wave] = dot[j];
+      }
+    }
+    if constexpr (WAVES > 1) {
+      __syncthreads();
+      const int j = threadIdx.x;
+      if (j < KK && j0 + j < k) grad_w[(size_t)at.t * k + j0 + j] = (part[j][0] + part[j][1]) + (part[j][2] + part[j][3]);
+      if constexpr (K == 0) __syncthreads();   // part is written again
+    }
+  }
+}
+
+// The weights of a token are the softmax of its kept logits, so d w_i / d logit_j = w_i (delta_ij - w_j) among them:
+// grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A thread takes 4 experts of a token.
+__global__ __launch_bounds__(256) void k_route_topk_grad(const int32_t* __restrict__ ids, const float* __restrict__ w,
+                                                         const float* __restrict__ gw, int64_t n_units, int E, int k, int quads,
+                                                         float* __restrict__ out) {
+  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (unit >= n_units) return;
+  const int64_t t = unit / quads;
+  const int e0 = (int)(unit - t * quads) * 4;
+  float sum = 0.f;
+  for (int j = 0; j < k; j++) sum = fmaf(gw[t * k + j], w[t * k + j], sum);
+  float o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < k; j++) {
+    const int e = ids[t * k + j] - e0;
+    const float d = w[t * k + j] * (gw[t * k + j] - sum);
+#pragma unroll
+    for (int c = 0; c < 4; c++) o[c] += e == c ? d : 0.f;
+  }
+#pragma unroll
+  for (int c = 0; c < 4; c++)
+    if (e0 + c < E) out[t * E + e0 + c] = o[c];
+}
+
+namespace {
+
+struct RowCall {
+  int T, k, R;
+  uint32_t row_bytes;
+  hipStream_t st;
+  size_t token_bytes() const { return (size_t)T * row_bytes; }
+  size_t rows_bytes() const { return (size_t)R * row_bytes; }
+};
+
+// Lanes of a token.
+int lanes_of(const RowCall& c) { return c.row_bytes <= 8 * 16 ? 8 : c.row_bytes <= 32 * 16 ? 32 : 64; }
+
+template <int LP, int NV>
+dim3 row_grid(const RowCall& c, int* spans) {
+  *spans = LP == 64 ? (int)((c.row_bytes + 64 * 16 * NV - 1) / (64 * 16 * NV)) : 1;
+  const int64_t waves = LP == 64 ? (int64_t)c.T * *spans : ((int64_t)c.T * LP + 63) / 64;
+  return dim3((unsigned)((waves + 3) / 4));
+}
+
+template <int LP, int NV>
+hipError_t dispatch_as(const RowCall& c, const void* x, const int32_t* inv, void* rows) {
+  int spans;
+  const dim3 grid = row_grid<LP, NV>(c, &spans);
+  hipLaunchKernelGGL((k_dispatch<LP, NV>), grid, dim3(256), 0, c.st, (const char*)x, inv, (char*)rows, c.T, c.k, c.R, c.row_bytes, spans);
+  return hipGetLastError();
+}
+hipError_t launch_dispatch(const RowCall& c, const void* x, const int32_t* inv, void* rows) {
+  switch (lanes_of(c)) {
+    case 8: return dispatch_as<8, 1>(c, x, inv, rows);
+    case 32: return dispatch_as<32, 1>(c, x, inv, rows);
+    default: return dispatch_as<64, 4>(c, x, inv, rows);
+  }
+}
+
+template <int DT, int K, int LP, int NV>
+hipError_t combine_as(const RowCall& c, const void* rows, const int32_t* inv, const float* w, void* out) {
+  int spans;
+  const dim3 grid = row_grid<LP, NV>(c, &spans);
+  hipLaunchKernelGGL((k_combine_rows<DT, K, LP, NV>), grid, dim3(256), 0, c.st, (const char*)rows, inv, w, (char*)out, c.T, c.k, c.R, c.row_bytes, spans);
+  return hipGetLastError();
+}
+template <int DT, int K>
+hipError_t combine_k(const RowCall& c, const void* rows, const int32_t* inv, const float* w, void* out) {
+  switch (lanes_of(c)) {
+    case 8: return combine_as<DT, K, 8, 1>(c, rows, inv, w, out);
+    case 32: return combine_as<DT, K, 32, 1>(c, rows, inv, w, out);
+    default: return combine_as<DT, K, 64, (K == 8 || K == 4) ? 2 : 4>(c, rows, inv, w, out);
+  }
+}
+template <int DT>
+hipError_t combine_type(const RowCall& c, const void* rows, const int32_t* inv, const float* w, void* out) {
+  if (c.k == 1) return combine_k<DT, 1>(c, rows, inv, w, out);
+  if (c.k == 2) return combine_k<DT, 2>(c, rows, inv, w, out);
+  if (c.k <= 4) return combine_k<DT, 4>(c, rows, inv, w, out);
+  if (c.k <= 8) return combine_k<DT, 8>(c, rows, inv, w, out);
+  return combine_k<DT, 0>(c, rows, inv, w, out);
+}
+hipError_t launch_combine_rows(int dtype, const RowCall& c, const void* rows, const int32_t* inv, const float* w, void* out) {
+  switch (dtype) {
+    case MOE_BF16: return combine_type<MOE_BF16>(c, rows, inv, w, out);
+    case MOE_FP16: return combine_type<MOE_FP16>(c, rows, inv, w, out);
+    default: return combine_type<MOE_FP32>(c, rows, inv, w, out);
+  }
+}
+
+template <int DT, int K, int LP, int NV, int WAVES>
+hipError_t combine_grad_as(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
+  const int64_t blocks = WAVES > 1 ? c.T : (((int64_t)c.T * LP + 63) / 64 + 3) / 4;
+  hipLaunchKernelGGL((k_combine_grad<DT, K, LP, NV, WAVES>), dim3((unsigned)blocks), dim3(256), 0, c.st, (const char*)g, (const char*)rows, inv, w,
+                     (char*)grad_rows, grad_w, c.T, c.k, c.R, c.row_bytes);
+  return hipGetLastError();
+}
+constexpr int kGradTokensPerWave = 4096;   // tokens from which a wavefront has one to itself
+template <int DT, int K>
+hipError_t combine_grad_k(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
+  constexpr int NV = K == 8 ? 1 : 2;
+  switch (lanes_of(c)) {
+    case 8: return combine_grad_as<DT, K, 8, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+    case 32: return combine_grad_as<DT, K, 32, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+    default:
+      if (c.T >= kGradTokensPerWave) return combine_grad_as<DT, K, 64, NV, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+      return combine_grad_as<DT, K, 64, NV, 4>(c, g, rows, inv, w, grad_rows, grad_w);
+  }
+}
+template <int DT>
+hipError_t combine_grad_type(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
+  if (c.k == 1) return combine_grad_k<DT, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+  if (c.k == 2) return combine_grad_k<DT, 2>(c, g, rows, inv, w, grad_rows, grad_w);
+  if (c.k <= 4) return combine_grad_k<DT, 4>(c, g, rows, inv, w, grad_rows, grad_w);
+  if (c.k <= 8) return combine_grad_k<DT, 8>(c, g, rows, inv, w, grad_rows, grad_w);
+  return combine_grad_k<DT, 0>(c, g, rows, inv, w, grad_rows, grad_w);
+}
+
+int n_chunks_of(int64_t R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
+constexpr int kSortOwnSums = 512;   // chunks up to which the scatter sums the counts itself
+
+// Checks that the row operators share; *c is set where there is something to do.
+int row_call(int32_t T, int32_t H, int32_t k, int32_t dtype, void* hip_stream, RowCall* c) {
+  if (T < 0 || H <= 0 || k <= 0 || element_bytes(dtype) == 0) return MOE_ERR_INVALID_ARG;
+  if (k > kMaxGateTopK || H < kMinRowColumns || H > kMaxRowColumns || (int64_t)T * k >= (1 << 24)) return MOE_ERR_UNSUPPORTED;
+  if ((int64_t)T * H * element_bytes(dtype) >= (1ll << 36)) return MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
+  c->T = T;
+  c->k = k;
+  c->R = T * k;
+  c->row_bytes = (uint32_t)(H * element_bytes(dtype));
+  c->st = (hipStream_t)hip_stream;
+  return MOE_OK;
+}
+
+int sort_shape(int32_t T, int32_t E, int32_t k) {
+  if (T < 0 || E <= 0 || k <= 0) return MOE_ERR_INVALID_ARG;
+  if (E > kMaxExperts || k > kMaxGateTopK || (int64_t)T * k >= (1 << 24)) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+int status_of(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
+
+}  // namespace
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+size_t moe_sort_workspace_bytes(int32_t T, int32_t E, int32_t k) {
+  if (sort_shape(T, E, k) != MOE_OK) return 0;
+  return ((size_t)n_chunks_of((int64_t)T * k) + 1) * (E + 1) * 4;
+}
+
+int moe_sort_tokens(const int32_t* topk_ids, int32_t T, int32_t E, int32_t k, int32_t* expert_offsets, int32_t* perm,
+                    int32_t* inv_perm, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = sort_shape(T, E, k);
+  if (rc != MOE_OK) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (!expert_offsets || !aligned16(expert_offsets)) return MOE_ERR_INVALID_ARG;
+  const int R = T * k;
+  if (R == 0) {
+    hipLaunchKernelGGL(k_sort_none, dim3(1), dim3(256), 0, st, E, expert_offsets);
+    return status_of(hipGetLastError());
+  }
+  if (!topk_ids || !perm || !inv_perm || !workspace) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(topk_ids) || !aligned16(perm) || !aligned16(inv_perm) || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
+  if (workspace_bytes < moe_sort_workspace_bytes(T, E, k)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  if (R <= kSortSmall) {
+    if (R <= 1024) hipLaunchKernelGGL((k_sort_small<16>), dim3(1), dim3(1024), 0, st, topk_ids, R, E, expert_offsets, perm, inv_perm);
+    else hipLaunchKernelGGL((k_sort_small<kSortSmall / 64>), dim3(1), dim3(1024), 0, st, topk_ids, R, E, expert_offsets, perm, inv_perm);
+    return status_of(hipGetLastError());
+  }
+  int32_t* hist = (int32_t*)workspace;
+  const int n_chunks = n_chunks_of(R);
+  int32_t* total = n_chunks > kSortOwnSums ? hist + (size_t)n_chunks * (E + 1) : nullptr;
+  hipLaunchKernelGGL(k_sort_hist, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist);
+  if (total) hipLaunchKernelGGL(k_sort_scan, dim3(E + 1), dim3(1024), 0, st, hist, n_chunks, E, total);
+  hipLaunchKernelGGL(k_sort_scatter, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist, n_chunks, total, expert_offsets, perm, inv_perm);
+  return status_of(hipGetLastError());
+}
+
+int moe_dispatch(const void* x, const int32_t* inv_perm, int32_t T, int32_t H, int32_t k, int32_t dtype, void* rows,
+                 void* hip_stream) {
+  RowCall c;
+  const int rc = row_call(T, H, k, dtype, hip_stream, &c);
+  if (rc != MOE_OK) return rc;
+  if (T == 0) return MOE_OK;
+  if (!x || !inv_perm || !rows || !aligned16(x) || !aligned16(inv_perm) || !aligned16(rows)) return MOE_ERR_INVALID_ARG;
+  if (overlap(x, c.token_bytes(), rows, c.rows_bytes())) return MOE_ERR_INVALID_ARG;
+  return status_of(launch_dispatch(c, x, inv_perm, rows));
+}
+
+int moe_combine(const void* rows, const int32_t* inv_perm, const float* topk_weights, int32_t T, int32_t H, int32_t k,
+                int32_t dtype, void* out, void* hip_stream) {
+  RowCall c;
+  const int rc = row_call(T, H, k, dtype, hip_stream, &c);
+  if (rc != MOE_OK) return rc;
+  if (T == 0) return MOE_OK;
+  if (!rows || !inv_perm || !out || !aligned16(rows) || !aligned16(inv_perm) || !aligned16(out) || !aligned16(topk_weights))
+    return MOE_ERR_INVALID_ARG;
+  if (overlap(rows, c.rows_bytes(), out, c.token_bytes())) return MOE_ERR_INVALID_ARG;
+  return status_of(launch_combine_rows(dtype, c, rows, inv_perm, topk_weights, out));
+}
+
+int moe_dispatch_backward(const void* grad_rows, const int32_t* inv_perm, int32_t T, int32_t H, int32_t k, int32_t dtype,
+                          void* grad_x, void* hip_stream) {
+  return moe_combine(grad_rows, inv_perm, nullptr, T, H, k, dtype, grad_x, hip_stream);
+}
+
+int moe_combine_backward(const void* grad_out, const void* rows, const int32_t* inv_perm, const float* topk_weights, int32_t T,
+                         int32_t H, int32_t k, int32_t dtype, void* grad_rows, float* grad_weights, void* hip_stream) {
+  RowCall c;
+  const int rc = row_call(T, H, k, dtype, hip_stream, &c);
+  if (rc != MOE_OK) return rc;
+  if (T == 0) return MOE_OK;
+  if (!grad_out || !inv_perm || !grad_rows || (grad_weights && !rows)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(grad_out) || !aligned16(rows) || !aligned16(inv_perm) || !aligned16(topk_weights) || !aligned16(grad_rows) ||
+      !aligned16(grad_weights))
+    return MOE_ERR_INVALID_ARG;
+  if (overlap(grad_out, c.token_bytes(), grad_rows, c.rows_bytes()) || (rows && overlap(rows, c.rows_bytes(), grad_rows, c.rows_bytes())))
+    return MOE_ERR_INVALID_ARG;
+  if (!grad_weights) rows = nullptr;
+  switch (dtype) {
+    case MOE_BF16: return status_of(combine_grad_type<MOE_BF16>(c, grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights));
+    case MOE_FP16: return status_of(combine_grad_type<MOE_FP16>(c, grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights));
+    default: return status_of(combine_grad_type<MOE_FP32>(c, grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights));
+  }
+}
+
+int moe_route_topk_backward(const int32_t* topk_ids, const float* topk_weights, const float* grad_weights, int32_t T, int32_t E,
+                            int32_t k, float* grad_logits, void* hip_stream) {
+  if (T < 0 || E <= 0 || k <= 0 || k > E) return MOE_ERR_INVALID_ARG;
+  if (E > kMaxExperts || k > kMaxGateTopK || (int64_t)T * k >= (1 << 24)) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  if (!topk_ids || !topk_weights || !grad_weights || !grad_logits) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(topk_ids) || !aligned16(topk_weights) || !aligned16(grad_weights) || !aligned16(grad_logits)) return MOE_ERR_INVALID_ARG;
+  const int quads = (E + 3) / 4;
+  const int64_t n_units = (int64_t)T * quads;
+  hipLaunchKernelGGL(k_route_topk_grad, dim3((unsigned)((n_units + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, topk_ids, topk_weights,
+                     grad_weights, n_units, E, k, quads, grad_logits);
+  return status_of(hipGetLastError());
+}
+
+}  // extern "C"
