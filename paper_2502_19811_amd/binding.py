@@ -294,10 +294,20 @@ def moe_probe_copy(dst, src, stream=None) -> float:
 
 # ---- operators around the experts ----
 # The C calls see addresses only, so what they cannot check is checked here: every tensor has the type and shape its call
-# says, is contiguous, and lies on the current device, as the stream does.
+# says, is contiguous, and lies on the current device, as the stream does.  These calls are often a few microseconds of work:
+# checking a tensor takes 0.3 us, and the current stream is asked for by its address (0.1 us; as an object 1.1).
 
-_DTYPES = {"torch.bfloat16": MOE_BF16, "torch.float16": MOE_FP16, "torch.float32": MOE_FP32}
-_INT32, _FLOAT32, _UINT8 = "torch.int32", "torch.float32", "torch.uint8"
+_DTYPES = {}            # torch's row types -> their numbers, filled at the first call
+_INT32 = _FLOAT32 = _UINT8 = _current_device = _raw_stream = None
+
+
+def _first_call() -> None:
+    global _INT32, _FLOAT32, _UINT8, _current_device, _raw_stream
+    import torch
+    _INT32, _FLOAT32, _UINT8 = torch.int32, torch.float32, torch.uint8
+    _current_device = torch.cuda.current_device
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _DTYPES.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
 
 
 class _Call:
@@ -306,32 +316,33 @@ class _Call:
     __slots__ = ("where", "device", "stream")
 
     def __init__(self, where: str, stream):
-        import torch
+        if _INT32 is None:
+            _first_call()
         self.where = where
-        self.device = torch.cuda.current_device()
+        self.device = _current_device()
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        elif stream.device_index != self.device:
+            self.stream = _raw_stream(self.device)
+        elif stream.device_index == self.device:
+            self.stream = stream.cuda_stream
+        else:
             self.refuse()
-        self.stream = stream.cuda_stream
 
     def refuse(self):
         raise MoEError(-1, self.where)
 
-    def arg(self, t, dtype: str, *shape) -> int:
-        if str(t.dtype) != dtype or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
+    def arg(self, t, dtype, shape) -> int:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
             self.refuse()
         return t.data_ptr()
 
-    def opt(self, t, dtype: str, *shape) -> Optional[int]:
-        return None if t is None else self.arg(t, dtype, *shape)
+    def opt(self, t, dtype, shape) -> Optional[int]:
+        return None if t is None else self.arg(t, dtype, shape)
 
     def rows(self, t):
-        """(T, H, type's name, its number) of a tensor of rows."""
-        name = str(t.dtype)
-        if t.dim() != 2 or name not in _DTYPES:
+        """(shape, type, its number) of a tensor of rows."""
+        if t.dim() != 2 or t.dtype not in _DTYPES:
             self.refuse()
-        return t.shape[0], t.shape[1], name, _DTYPES[name]
+        return t.shape, t.dtype, _DTYPES[t.dtype]
 
     def pairs(self, t):
         """(T, k) of a tensor of pairs."""
@@ -342,7 +353,7 @@ class _Call:
     def workspace(self, t):
         if t is None:
             return None, 0
-        return self.arg(t, _UINT8, t.numel()), t.numel()
+        return self.arg(t, _UINT8, (t.numel(),)), t.numel()
 
     def done(self, status: int) -> None:
         if status != 0:
@@ -356,52 +367,57 @@ def moe_sort_workspace_bytes(T: int, E: int, k: int) -> int:
 def moe_sort_tokens(topk_ids, E: int, expert_offsets, perm, inv_perm, workspace, stream=None) -> None:
     """topk_ids int32 [T,k] -> expert_offsets int32 [E+1], perm int32 [T*k], inv_perm int32 [T,k]; workspace uint8."""
     c = _Call("moe_sort_tokens", stream)
-    T, k = c.pairs(topk_ids)
+    T, k = pairs = c.pairs(topk_ids)
     c.done(load_library().moe_sort_tokens(
-        c.arg(topk_ids, _INT32, T, k), T, E, k, c.arg(expert_offsets, _INT32, E + 1), c.arg(perm, _INT32, T * k),
-        c.arg(inv_perm, _INT32, T, k), *c.workspace(workspace), c.stream))
+        c.arg(topk_ids, _INT32, pairs), T, E, k, c.arg(expert_offsets, _INT32, (E + 1,)), c.arg(perm, _INT32, (T * k,)),
+        c.arg(inv_perm, _INT32, pairs), *c.workspace(workspace), c.stream))
 
 
 def moe_dispatch(x, inv_perm, rows, stream=None) -> None:
     """x [T,H], inv_perm int32 [T,k] -> rows [T*k,H]."""
     c = _Call("moe_dispatch", stream)
-    (T, H, name, dtype), k = c.rows(x), c.pairs(inv_perm)[1]
-    c.done(load_library().moe_dispatch(c.arg(x, name, T, H), c.arg(inv_perm, _INT32, T, k), T, H, k, dtype,
-                                       c.arg(rows, name, T * k, H), c.stream))
+    (T, H), t, dtype = c.rows(x)
+    k = c.pairs(inv_perm)[1]
+    c.done(load_library().moe_dispatch(c.arg(x, t, (T, H)), c.arg(inv_perm, _INT32, (T, k)), T, H, k, dtype, c.arg(rows, t, (T * k, H)), c.stream))
 
 
 def moe_dispatch_backward(grad_rows, inv_perm, grad_x, stream=None) -> None:
     """grad_rows [T*k,H], inv_perm int32 [T,k] -> grad_x [T,H]."""
     c = _Call("moe_dispatch_backward", stream)
-    (T, H, name, dtype), k = c.rows(grad_x), c.pairs(inv_perm)[1]
-    c.done(load_library().moe_dispatch_backward(c.arg(grad_rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), T, H, k, dtype,
-                                                c.arg(grad_x, name, T, H), c.stream))
+    (T, H), t, dtype = c.rows(grad_x)
+    k = c.pairs(inv_perm)[1]
+    c.done(load_library().moe_dispatch_backward(c.arg(grad_rows, t, (T * k, H)), c.arg(inv_perm, _INT32, (T, k)), T, H, k, dtype,
+                                                c.arg(grad_x, t, (T, H)), c.stream))
 
 
 def moe_combine(rows, inv_perm, topk_weights, out, stream=None) -> None:
     """rows [T*k,H], inv_perm int32 [T,k], topk_weights fp32 [T,k] or None -> out [T,H]."""
     c = _Call("moe_combine", stream)
-    (T, H, name, dtype), k = c.rows(out), c.pairs(inv_perm)[1]
-    c.done(load_library().moe_combine(c.arg(rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), c.opt(topk_weights, _FLOAT32, T, k),
-                                      T, H, k, dtype, c.arg(out, name, T, H), c.stream))
+    (T, H), t, dtype = c.rows(out)
+    k = c.pairs(inv_perm)[1]
+    c.done(load_library().moe_combine(c.arg(rows, t, (T * k, H)), c.arg(inv_perm, _INT32, (T, k)), c.opt(topk_weights, _FLOAT32, (T, k)),
+                                      T, H, k, dtype, c.arg(out, t, (T, H)), c.stream))
 
 
 def moe_combine_backward(grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights, stream=None) -> None:
     """grad_out [T,H], rows [T*k,H] -> grad_rows [T*k,H], grad_weights fp32 [T,k] (None: not wanted, rows may be None)."""
     c = _Call("moe_combine_backward", stream)
-    (T, H, name, dtype), k = c.rows(grad_out), c.pairs(inv_perm)[1]
+    (T, H), t, dtype = c.rows(grad_out)
+    k = c.pairs(inv_perm)[1]
+    pairs, all_rows = (T, k), (T * k, H)
     c.done(load_library().moe_combine_backward(
-        c.arg(grad_out, name, T, H), c.opt(rows, name, T * k, H), c.arg(inv_perm, _INT32, T, k), c.opt(topk_weights, _FLOAT32, T, k),
-        T, H, k, dtype, c.arg(grad_rows, name, T * k, H), c.opt(grad_weights, _FLOAT32, T, k), c.stream))
+        c.arg(grad_out, t, (T, H)), c.opt(rows, t, all_rows), c.arg(inv_perm, _INT32, pairs), c.opt(topk_weights, _FLOAT32, pairs),
+        T, H, k, dtype, c.arg(grad_rows, t, all_rows), c.opt(grad_weights, _FLOAT32, pairs), c.stream))
 
 
 def moe_route_topk_backward(topk_ids, topk_weights, grad_weights, grad_logits, stream=None) -> None:
     """topk_ids int32 [T,k], topk_weights and grad_weights fp32 [T,k] -> grad_logits fp32 [T,E]."""
     c = _Call("moe_route_topk_backward", stream)
-    (T, k), E = c.pairs(topk_ids), c.pairs(grad_logits)[1]
+    T, k = pairs = c.pairs(topk_ids)
+    E = c.pairs(grad_logits)[1]
     c.done(load_library().moe_route_topk_backward(
-        c.arg(topk_ids, _INT32, T, k), c.arg(topk_weights, _FLOAT32, T, k), c.arg(grad_weights, _FLOAT32, T, k), T, E, k,
-        c.arg(grad_logits, _FLOAT32, T, E), c.stream))
+        c.arg(topk_ids, _INT32, pairs), c.arg(topk_weights, _FLOAT32, pairs), c.arg(grad_weights, _FLOAT32, pairs), T, E, k,
+        c.arg(grad_logits, _FLOAT32, (T, E)), c.stream))
 
 
 def moe_norm_workspace_bytes(T: int, H: int) -> int:
@@ -411,51 +427,52 @@ def moe_norm_workspace_bytes(T: int, H: int) -> int:
 def moe_norm_before(residual, update, residual_scale: float, gamma, beta, norm: int, eps: float, sum, x, stream=None) -> None:
     """sum = residual + residual_scale * update, x = norm of it; update, beta and sum may be None."""
     c = _Call("moe_norm_before", stream)
-    T, H, name, dtype = c.rows(residual)
+    s, t, dtype = c.rows(residual)
+    T, H = s
     c.done(load_library().moe_norm_before(
-        c.arg(residual, name, T, H), c.opt(update, name, T, H), residual_scale, c.arg(gamma, name, H), c.opt(beta, name, H), norm, eps,
-        T, H, dtype, c.opt(sum, name, T, H), c.arg(x, name, T, H), c.stream))
+        c.arg(residual, t, s), c.opt(update, t, s), residual_scale, c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), norm, eps, T, H, dtype,
+        c.opt(sum, t, s), c.arg(x, t, s), c.stream))
 
 
 def moe_norm_before_backward(sum, gamma, grad_x, grad_sum, residual_scale: float, norm: int, eps: float, grad_residual, grad_update,
                              grad_gamma, grad_beta, workspace, stream=None) -> None:
     """grad_sum, grad_update, grad_gamma and grad_beta may be None; without the last two workspace may be, too."""
     c = _Call("moe_norm_before_backward", stream)
-    T, H, name, dtype = c.rows(sum)
+    s, t, dtype = c.rows(sum)
+    T, H = s
     c.done(load_library().moe_norm_before_backward(
-        c.arg(sum, name, T, H), c.arg(gamma, name, H), c.arg(grad_x, name, T, H), c.opt(grad_sum, name, T, H), residual_scale, norm, eps,
-        T, H, dtype, c.arg(grad_residual, name, T, H), c.opt(grad_update, name, T, H), c.opt(grad_gamma, _FLOAT32, H),
-        c.opt(grad_beta, _FLOAT32, H), *c.workspace(workspace), c.stream))
+        c.arg(sum, t, s), c.arg(gamma, t, (H,)), c.arg(grad_x, t, s), c.opt(grad_sum, t, s), residual_scale, norm, eps, T, H, dtype,
+        c.arg(grad_residual, t, s), c.opt(grad_update, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),
+        *c.workspace(workspace), c.stream))
 
 
-def _gate(c: _Call, gate, kind: int, T: int, H: int, name: str) -> Optional[int]:
-    """A gate of this kind; name: type of a channel or full one."""
+def _gate(c: _Call, gate, kind: int, shape, t) -> Optional[int]:
+    """A gate of this kind; shape: of the rows; t: type of a channel or full one."""
     if gate is None:
         return None
-    if kind == MOE_GATE_CHANNEL:
-        return c.arg(gate, name, H)
     if kind == MOE_GATE_TOKEN:
-        return c.arg(gate, _FLOAT32, T)
-    return c.arg(gate, name, T, H)
+        return c.arg(gate, _FLOAT32, shape[:1])
+    return c.arg(gate, t, shape[1:] if kind == MOE_GATE_CHANNEL else shape)
 
 
 def moe_norm_after(residual, y, gamma, beta, gate, gate_kind: int, residual_scale: float, norm: int, eps: float, out,
                    stream=None) -> None:
     """out = residual + residual_scale * gate * norm of y; residual and beta may be None, gate is with MOE_GATE_NONE."""
     c = _Call("moe_norm_after", stream)
-    T, H, name, dtype = c.rows(y)
+    s, t, dtype = c.rows(y)
+    T, H = s
     c.done(load_library().moe_norm_after(
-        c.opt(residual, name, T, H), c.arg(y, name, T, H), c.arg(gamma, name, H), c.opt(beta, name, H),
-        _gate(c, gate, gate_kind, T, H, name), gate_kind, residual_scale, norm, eps, T, H, dtype, c.arg(out, name, T, H), c.stream))
+        c.opt(residual, t, s), c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind,
+        residual_scale, norm, eps, T, H, dtype, c.arg(out, t, s), c.stream))
 
 
 def moe_norm_after_backward(y, gamma, beta, gate, gate_kind: int, residual_scale: float, grad_out, norm: int, eps: float, grad_y,
                             grad_gamma, grad_beta, grad_gate, workspace, stream=None) -> None:
     """grad_gamma, grad_beta and grad_gate may be None; workspace too if nothing is summed over tokens."""
     c = _Call("moe_norm_after_backward", stream)
-    T, H, name, dtype = c.rows(y)
+    s, t, dtype = c.rows(y)
+    T, H = s
     c.done(load_library().moe_norm_after_backward(
-        c.arg(y, name, T, H), c.arg(gamma, name, H), c.opt(beta, name, H), _gate(c, gate, gate_kind, T, H, name), gate_kind,
-        residual_scale, c.arg(grad_out, name, T, H), norm, eps, T, H, dtype, c.arg(grad_y, name, T, H), c.opt(grad_gamma, _FLOAT32, H),
-        c.opt(grad_beta, _FLOAT32, H), _gate(c, grad_gate, gate_kind, T, H, _FLOAT32 if gate_kind == MOE_GATE_CHANNEL else name),
-        *c.workspace(workspace), c.stream))
+        c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind, residual_scale,
+        c.arg(grad_out, t, s), norm, eps, T, H, dtype, c.arg(grad_y, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),
+        _gate(c, grad_gate, gate_kind, s, _FLOAT32 if gate_kind == MOE_GATE_CHANNEL else t), *c.workspace(workspace), c.stream))
