@@ -33,7 +33,7 @@ struct NormGradParams {
   char* grad_v;
   char* grad_other;       // before: scale * grad_v, or nullptr; after: gradient of a full gate, or nullptr
   float* grad_token_gate; // after: gradient of a token gate, or nullptr
-  float* part_a;          // [groups][H] sums over the rows of a group, or nullptr
+  float* part_a;          // [workgroups][H] sums over the rows of a workgroup, or nullptr
   float* part_b;
   int32_t gate_kind, layer, T, H, groups;
   uint32_t row_bytes;
@@ -69,6 +69,26 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int which, bool ragged) 
 template <int W> constexpr int threads_of() { return W > 4 ? W * 64 : 256; }
 template <int W> constexpr int rows_of() { return W > 4 ? 1 : 4 / W; }   // rows of a workgroup
 
+// Runs body(piece, column, counts) over a lane's elements; counts is false for those that are another lane's, too, or nobody's.
+template <int NV, int N, int UNIT, typename F>
+__device__ __forceinline__ void each_counted(const uint32_t (&at)[NV], uint32_t row_bytes, bool exact, F body) {
+  if (exact) {
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int c = 0; c < N; c++) body(i, c, true);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int from = counted<UNIT>(at[i], row_bytes);
+#pragma unroll
+      for (int c = 0; c < N; c++) body(i, c, c >= from);
+    }
+  }
+}
+
+// n = v * r - mean * r, one fused operation an element whatever the norm: at 16 lanes a cycle and SIMD an operation on every element of
+// 16384 x 4096 takes 1.7 us, so the gradients, which read three rows, have room for about 30.
 template <int DT, int W, int NV, bool AFTER>
 __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   using V = Row<DT>;
@@ -84,18 +104,19 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   u32x4 rv[NV], bv[NV], gv[NV], hv[NV];
   if (!AFTER || p.residual != nullptr)
 #pragma unroll
-    for (int i = 0; i < NV; i++) rv[i] = load_piece(p.residual + row, at[i], p.row_bytes);
+    for (int i = 0; i < NV; i++) rv[i] = load_once(p.residual + row, at[i], p.row_bytes);
   if (AFTER || p.branch != nullptr)
 #pragma unroll
-    for (int i = 0; i < NV; i++) bv[i] = load_piece(p.branch + row, at[i], p.row_bytes);
-  float gate_t = 1.f;
+    for (int i = 0; i < NV; i++) bv[i] = load_once(p.branch + row, at[i], p.row_bytes);
+  float scale = p.scale;
+  const bool gated = AFTER && (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL);
   if constexpr (AFTER) {
-    if (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL) {
+    if (gated) {
       const char* gate = p.gate + (p.gate_kind == MOE_GATE_FULL ? row : 0);
 #pragma unroll
       for (int i = 0; i < NV; i++) hv[i] = load_piece(gate, at[i], p.row_bytes);
     } else if (p.gate_kind == MOE_GATE_TOKEN) {
-      gate_t = ((const float*)p.gate)[t];
+      scale *= ((const float*)p.gate)[t];
     }
   }
 #pragma unroll
@@ -118,44 +139,38 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   float mean = 0.f, sq[1] = {0.f};
   if (p.layer) {
     float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-      const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
-#pragma unroll
-      for (int c = 0; c < N; c++) s[0] += exact || c >= from ? v[i][c] : 0.f;
-    }
+    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) { s[0] += counts ? v[i][c] : 0.f; });
     row_sums<W>(s, 0, false);
     mean = s[0] * p.inv_h;
-  }
-#pragma unroll
-  for (int i = 0; i < NV; i++) {
-    const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
-#pragma unroll
-    for (int c = 0; c < N; c++) {
-      const float d = v[i][c] - mean;
-      sq[0] = exact || c >= from ? fmaf(d, d, sq[0]) : sq[0];
-    }
+    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+      const float d = counts ? v[i][c] - mean : 0.f;
+      sq[0] = fmaf(d, d, sq[0]);
+    });
+  } else {
+    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+      const float d = counts ? v[i][c] : 0.f;
+      sq[0] = fmaf(d, d, sq[0]);
+    });
   }
   row_sums<W>(sq, 1, ragged);
-  const float r = 1.f / sqrtf(fmaf(sq[0], p.inv_h, p.eps));
+  const float r = 1.f / sqrtf(fmaf(sq[0], p.inv_h, p.eps)), minus = p.layer ? -mean * r : 0.f;
   if constexpr (!AFTER)
     if (p.sum != nullptr)
 #pragma unroll
-      for (int i = 0; i < NV; i++) store_piece(p.sum + row, at[i], p.row_bytes, V::pack(v[i]));
+      for (int i = 0; i < NV; i++) store_once(p.sum + row, at[i], p.row_bytes, V::pack(v[i]));
 #pragma unroll
   for (int i = 0; i < NV; i++) {
     float o[N], f[N];
     V::unpack(gv[i], f);
 #pragma unroll
-    for (int c = 0; c < N; c++) o[c] = (v[i][c] - mean) * r * f[c];
+    for (int c = 0; c < N; c++) o[c] = fmaf(v[i][c], r, minus) * f[c];
     if (p.beta != nullptr) {
       V::unpack(load_piece(p.beta, at[i], p.row_bytes), f);
 #pragma unroll
       for (int c = 0; c < N; c++) o[c] += f[c];
     }
     if constexpr (AFTER) {
-      const float m = p.scale * gate_t;
-      if (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL) {
+      if (gated) {
         V::unpack(hv[i], f);
 #pragma unroll
         for (int c = 0; c < N; c++) o[c] *= f[c];
@@ -164,41 +179,45 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
       for (int c = 0; c < N; c++) f[c] = 0.f;
       if (p.residual != nullptr) V::unpack(rv[i], f);
 #pragma unroll
-      for (int c = 0; c < N; c++) o[c] = fmaf(m, o[c], f[c]);
+      for (int c = 0; c < N; c++) o[c] = fmaf(scale, o[c], f[c]);
     }
     store_piece(p.out + row, at[i], p.row_bytes, V::pack(o));
   }
 }
 
 // Gradients.  With n the normed row, e the gradient of n and r the reciprocal deviation, the gradient of the row is
-//   r * (e - mean(e) - n * mean(e * n))           (without the mean of e where no mean was taken off).
+//   r * (e - mean(e) - n * mean(e * n))           (without the mean of e where no mean was taken off),
+// which is c1 * e + c2 * v + c0 with three numbers a row.  The scale and a token's gate are factors of these numbers.
 // A group of W wavefronts takes rows group, group + groups, ... and keeps, in registers, its columns' sums over them: A of
-// m * n and B of m, m the gradient of gamma * n + beta; they go to part_a and part_b, whose rows k_norm_columns adds up in a
-// fixed order.  A channel gate is a factor of these sums and joins there.  The next row is requested before the present one
+// f * n and B of f, f the gradient of gamma * n + beta but for the scale and a channel gate, which are factors of the sums; they go
+// to part_a and part_b, a row for each workgroup, which k_norm_columns adds up in a fixed order.  The next row is requested before the present one
 // is summed up (PRE), which the largest rows have no registers for.
-template <int DT, int W, int NV, bool AFTER, bool WITH_B, bool PRE>
+enum { GRAD_BEFORE = 0, GRAD_AFTER = 1, GRAD_AFTER_TOKEN = 2, GRAD_AFTER_FULL = 3 };   // AFTER: no gate or a channel gate
+template <int DT, int W, int NV, int MODE, bool WITH_B, bool PRE>
 __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p) {
   using V = Row<DT>;
   constexpr int N = V::kVec;
+  constexpr bool kToken = MODE == GRAD_AFTER_TOKEN, kFull = MODE == GRAD_AFTER_FULL;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int group = blockIdx.x * rows_of<W>() + wave / W;
-  if (group >= p.groups) return;   // (W > 1: the whole workgroup or nobody)
   const bool exact = p.row_bytes == W * NV * 1024, ragged = p.row_bytes % 16 != 0;
   uint32_t at[NV];
 #pragma unroll
   for (int i = 0; i < NV; i++) at[i] = (uint32_t)((i * W + wave % W) * 64 + lane) * 16;
-  u32x4 gamma[NV], beta[NV], chan[NV];
-  const bool has_beta = AFTER && p.beta != nullptr, channel = AFTER && p.gate_kind == MOE_GATE_CHANNEL;
-  const bool full = AFTER && p.gate_kind == MOE_GATE_FULL, token = AFTER && p.gate_kind == MOE_GATE_TOKEN;
+  float gamma[NV][N];   // with a channel gate multiplied in
+  u32x4 beta[NV];
+  const bool has_beta = (kToken || kFull) && p.beta != nullptr;
 #pragma unroll
-  for (int i = 0; i < NV; i++) gamma[i] = load_piece(p.gamma, at[i], p.row_bytes);
-  if constexpr (AFTER) {
-    if (has_beta)
+  for (int i = 0; i < NV; i++) {
+    V::unpack(load_piece(p.gamma, at[i], p.row_bytes), gamma[i]);
+    if constexpr (MODE == GRAD_AFTER)
+      if (p.gate_kind == MOE_GATE_CHANNEL) {
+        float h[N];
+        V::unpack(load_piece(p.gate, at[i], p.row_bytes), h);
 #pragma unroll
-      for (int i = 0; i < NV; i++) beta[i] = load_piece(p.beta, at[i], p.row_bytes);
-    if (channel)
-#pragma unroll
-      for (int i = 0; i < NV; i++) chan[i] = load_piece(p.gate, at[i], p.row_bytes);
+        for (int c = 0; c < N; c++) gamma[i][c] *= h[c];
+      }
+    if (has_beta) beta[i] = load_piece(p.beta, at[i], p.row_bytes);
   }
   float acc_a[NV][N], acc_b[WITH_B ? NV : 1][N];
 #pragma unroll
@@ -208,153 +227,153 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
       acc_a[i][c] = 0.f;
       if constexpr (WITH_B) acc_b[i][c] = 0.f;
     }
-  const char* third = AFTER ? (full ? p.gate : nullptr) : p.more;   // the third row that is read, if any
-  u32x4 vv[NV], gg[NV], mm[NV];
+  u32x4 vv[NV], gg[NV], hh[kFull ? NV : 1];
   auto request = [&](int t) {
     const size_t row = (size_t)t * p.row_bytes;
 #pragma unroll
-    for (int i = 0; i < NV; i++) vv[i] = load_piece(p.v + row, at[i], p.row_bytes);
+    for (int i = 0; i < NV; i++) vv[i] = load_once(p.v + row, at[i], p.row_bytes);
 #pragma unroll
-    for (int i = 0; i < NV; i++) gg[i] = load_piece(p.g + row, at[i], p.row_bytes);
-    if (third != nullptr)
+    for (int i = 0; i < NV; i++) gg[i] = load_once(p.g + row, at[i], p.row_bytes);
+    if constexpr (kFull)
 #pragma unroll
-      for (int i = 0; i < NV; i++) mm[i] = load_piece(third + row, at[i], p.row_bytes);
+      for (int i = 0; i < NV; i++) hh[i] = load_once(p.gate + row, at[i], p.row_bytes);
   };
   int flip = 0;
-  if constexpr (PRE) request(group);
+  if constexpr (PRE)
+    if (group < p.T) request(group);
   for (int t = group; t < p.T; t += p.groups) {
     const size_t row = (size_t)t * p.row_bytes;
     if constexpr (!PRE) request(t);
-    float v[NV][N];
-    u32x4 g[NV], m[NV];
+    u32x4 more[NV];   // what the stream's gradient is before
+    if constexpr (MODE == GRAD_BEFORE)
+      if (p.more != nullptr)
+#pragma unroll
+        for (int i = 0; i < NV; i++) more[i] = load_once(p.more + row, at[i], p.row_bytes);
+    float v[NV][N], f[NV][N], g[kFull ? NV : 1][N];   // f: gradient of gamma * n + beta, but for the factors said above
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       V::unpack(vv[i], v[i]);
-      g[i] = gg[i];
-      m[i] = mm[i];
+      V::unpack(gg[i], f[i]);
+      if constexpr (kFull) {
+        float h[N];
+        V::unpack(hh[i], h);
+#pragma unroll
+        for (int c = 0; c < N; c++) {
+          g[i][c] = f[i][c];
+          f[i][c] *= h[c];
+        }
+      }
     }
     if constexpr (PRE)
       if (t + p.groups < p.T) request(t + p.groups);
-    const float gate_t = token ? ((const float*)p.gate)[t] : 1.f;
-    // f: gradient of gamma * n + beta without a token gate or a channel gate; e: of n, without a token gate
-    auto gradients = [&](int i, float (&f)[N], float (&e)[N]) {
-      float x[N];
-      V::unpack(g[i], f);
-      if constexpr (AFTER) {
-#pragma unroll
-        for (int c = 0; c < N; c++) f[c] *= p.scale;
-        if (full) {
-          V::unpack(m[i], x);
-#pragma unroll
-          for (int c = 0; c < N; c++) f[c] *= x[c];
-        }
-      }
-      V::unpack(gamma[i], x);
-#pragma unroll
-      for (int c = 0; c < N; c++) e[c] = f[c] * x[c];
-      if constexpr (AFTER)
-        if (channel) {
-          V::unpack(chan[i], x);
-#pragma unroll
-          for (int c = 0; c < N; c++) e[c] *= x[c];
-        }
-    };
-    float mean = 0.f, mean_e = 0.f;
+    const float gate_t = kToken ? ((const float*)p.gate)[t] : 1.f;
+    float mean = 0.f, sum_e = 0.f;
+    float s[3] = {0.f, 0.f, 0.f};   // sums of the squares, of e * (v - mean), of f * beta
     if (p.layer) {
-      float s[2] = {0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NV; i++) {
-        const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
-        float f[N], e[N];
-        gradients(i, f, e);
-#pragma unroll
-        for (int c = 0; c < N; c++) {
-          s[0] += exact || c >= from ? v[i][c] : 0.f;
-          s[1] += exact || c >= from ? e[c] : 0.f;
-        }
-      }
-      row_sums<W>(s, flip, false);
-      mean = s[0] * p.inv_h;
-      mean_e = s[1] * p.inv_h;
+      float m[2] = {0.f, 0.f};
+      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+        m[0] += counts ? v[i][c] : 0.f;
+        m[1] += counts ? f[i][c] * gamma[i][c] : 0.f;
+      });
+      row_sums<W>(m, flip, false);
+      mean = m[0] * p.inv_h;
+      sum_e = m[1];
+      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+        const float d = counts ? v[i][c] - mean : 0.f;
+        s[0] = fmaf(d, d, s[0]);
+        s[1] = fmaf(counts ? f[i][c] * gamma[i][c] : 0.f, d, s[1]);
+      });
+    } else {
+      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+        const float d = counts ? v[i][c] : 0.f;
+        s[0] = fmaf(d, d, s[0]);
+        s[1] = fmaf(counts ? f[i][c] * gamma[i][c] : 0.f, d, s[1]);
+      });
     }
-    float s[3] = {0.f, 0.f, 0.f};
+    if constexpr (kToken)
+      if (has_beta) {
+        float b[NV][N];
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-      const int from = exact ? 0 : counted<V::kBytes>(at[i], p.row_bytes);
-      float f[N], e[N];
-      gradients(i, f, e);
-#pragma unroll
-      for (int c = 0; c < N; c++) {
-        const float d = v[i][c] - mean;
-        v[i][c] = d;
-        s[0] = exact || c >= from ? fmaf(d, d, s[0]) : s[0];
-        s[1] = exact || c >= from ? fmaf(e[c], d, s[1]) : s[1];
+        for (int i = 0; i < NV; i++) V::unpack(beta[i], b[i]);
+        each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) { s[2] += counts ? f[i][c] * b[i][c] : 0.f; });
       }
-      if (token && has_beta) {
-        float b[N];
-        V::unpack(beta[i], b);
-#pragma unroll
-        for (int c = 0; c < N; c++) s[2] = exact || c >= from ? fmaf(f[c], b[c], s[2]) : s[2];
-      }
-    }
     row_sums<W>(s, flip, ragged);
     flip ^= 1;
-    const float r = 1.f / sqrtf(fmaf(s[0], p.inv_h, p.eps));
+    const float r = 1.f / sqrtf(fmaf(s[0], p.inv_h, p.eps)), minus = p.layer ? -mean * r : 0.f;
     const float en = s[1] * r;   // sum of e * n
-    if (token && p.grad_token_gate != nullptr && lane == 0 && wave % W == 0) p.grad_token_gate[t] = en + s[2];
-    const float mean_en = en * p.inv_h;
+    if constexpr (kToken)
+      if (p.grad_token_gate != nullptr && lane == 0 && wave % W == 0) p.grad_token_gate[t] = p.scale * (en + s[2]);
+    const float c1 = MODE == GRAD_BEFORE ? r : r * p.scale * gate_t;
+    const float c2 = -c1 * r * (en * p.inv_h);
+    const float c0 = p.layer ? -c1 * (sum_e * p.inv_h) - c2 * mean : 0.f;
+    const float rt = kToken ? r * gate_t : r, minus_t = kToken ? minus * gate_t : minus;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      float f[N], e[N], o[N];
-      gradients(i, f, e);
+      float o[N], x[N];
+      if constexpr (MODE == GRAD_BEFORE) {
+#pragma unroll
+        for (int c = 0; c < N; c++) x[c] = 0.f;
+        if (p.more != nullptr) V::unpack(more[i], x);
+      }
 #pragma unroll
       for (int c = 0; c < N; c++) {
-        const float n = v[i][c] * r;
-        const float fc = f[c] * gate_t;
-        acc_a[i][c] = fmaf(fc, n, acc_a[i][c]);
-        if constexpr (WITH_B) acc_b[i][c] += fc;
-        o[c] = r * gate_t * (e[c] - mean_e - n * mean_en);
+        acc_a[i][c] = fmaf(f[i][c], fmaf(v[i][c], rt, minus_t), acc_a[i][c]);
+        if constexpr (WITH_B) acc_b[i][c] = fmaf(f[i][c], gate_t, acc_b[i][c]);
+        o[c] = fmaf(c1, f[i][c] * gamma[i][c], fmaf(c2, v[i][c], c0));
+        if constexpr (MODE == GRAD_BEFORE) o[c] += x[c];
       }
-      if constexpr (!AFTER) {
-        if (p.more != nullptr) {
-          float x[N];
-          V::unpack(m[i], x);
-#pragma unroll
-          for (int c = 0; c < N; c++) o[c] += x[c];
-        }
-        store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
+      store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
+      if constexpr (MODE == GRAD_BEFORE) {
         if (p.grad_other != nullptr) {
 #pragma unroll
           for (int c = 0; c < N; c++) o[c] *= p.scale;
           store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
         }
-      } else {
-        store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
-        if (full && p.grad_other != nullptr) {
-          float x[N], b[N];
-          V::unpack(gamma[i], x);
+      }
+      if constexpr (kFull) {
+        if (p.grad_other != nullptr) {
 #pragma unroll
-          for (int c = 0; c < N; c++) b[c] = 0.f;
-          if (has_beta) V::unpack(beta[i], b);
-          V::unpack(g[i], f);
+          for (int c = 0; c < N; c++) x[c] = 0.f;
+          if (has_beta) V::unpack(beta[i], x);
 #pragma unroll
-          for (int c = 0; c < N; c++) o[c] = p.scale * f[c] * fmaf(v[i][c] * r, x[c], b[c]);
+          for (int c = 0; c < N; c++) o[c] = p.scale * g[i][c] * fmaf(fmaf(v[i][c], r, minus), gamma[i][c], x[c]);
           store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
         }
       }
     }
   }
   if (p.part_a == nullptr) return;
+  const float scale = MODE == GRAD_BEFORE ? 1.f : p.scale;
+  auto leave = [&](float* part, float (&acc)[NV][N]) {
+    if constexpr (W > 1) {
 #pragma unroll
-  for (int i = 0; i < NV; i++) {
-    if (at[i] >= p.row_bytes) continue;
-    const size_t col = (size_t)group * p.H + piece_at(at[i], p.row_bytes) / V::kBytes;
+      for (int i = 0; i < NV; i++) {
+        if (at[i] >= p.row_bytes) continue;
+        const size_t col = (size_t)blockIdx.x * p.H + piece_at(at[i], p.row_bytes) / V::kBytes;
 #pragma unroll
-    for (int c = 0; c < N; c++) {
-      p.part_a[col + c] = acc_a[i][c];
-      if constexpr (WITH_B) p.part_b[col + c] = acc_b[i][c];
+        for (int c = 0; c < N; c++) part[col + c] = acc[i][c] * scale;
+      }
+    } else {
+      // the four groups of the workgroup meet in LDS, a quarter of the columns a wavefront
+      __shared__ float all[4][NV * N][64];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int c = 0; c < N; c++) all[wave][i * N + c][lane] = acc[i][c];
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < NV * N / 4; q++) {
+        const int ic = wave * (NV * N / 4) + q;
+        const uint32_t start = (uint32_t)(ic / N * 64 + lane) * 16;
+        if (start >= p.row_bytes) continue;
+        const size_t col = (size_t)blockIdx.x * p.H + piece_at(start, p.row_bytes) / V::kBytes + ic % N;
+        part[col] = ((all[0][ic][lane] + all[1][ic][lane]) + (all[2][ic][lane] + all[3][ic][lane])) * scale;
+      }
     }
-  }
+  };
+  leave(p.part_a, acc_a);
+  if constexpr (WITH_B) leave(p.part_b, acc_b);
 }
 
 struct NormColumnParams {
@@ -366,7 +385,7 @@ struct NormColumnParams {
   float* grad_gamma;      // each or nullptr
   float* grad_beta;
   float* grad_gate;
-  int32_t groups, H;
+  int32_t groups, H;      // rows of part_a and part_b, columns
 };
 
 // Column sums over the groups: a workgroup takes 32 columns, 32 threads each, which go down the groups in turn and meet in LDS.
@@ -405,13 +424,19 @@ __global__ __launch_bounds__(1024) void k_norm_columns(NormColumnParams p) {
 
 namespace {
 
-constexpr int kGroups1 = 2048, kGroups4 = 512, kGroups8 = 256;   // groups of rows, with 1, 4, and 8 or 16 wavefronts a row
+// Groups of rows at most, with 1, 4, and 8 or 16 wavefronts a row: what fits the device at a time.
+constexpr int kGroups1 = 4096, kGroups4 = 512, kGroups8 = 256;
 
-// Wavefronts that hold a row, from its pieces of 16 bytes, and pieces a lane.
-int waves_of(uint32_t pieces) { return pieces <= 256 ? 1 : pieces <= 512 ? 4 : pieces <= 1024 ? 8 : 16; }
+// Wavefronts that hold a row, from its pieces of 16 bytes.
+int waves_of(uint32_t pieces) { return pieces <= 128 ? 1 : pieces <= 512 ? 4 : pieces <= 1024 ? 8 : 16; }
 int groups_of(int T, uint32_t pieces) {
   const int waves = waves_of(pieces), most = waves == 1 ? kGroups1 : waves == 4 ? kGroups4 : kGroups8;
   return T < most ? T : most;
+}
+// Workgroups of the gradients, each of which leaves a row of column sums.
+int workgroups_of(int T, uint32_t pieces) {
+  const int groups = groups_of(T, pieces);
+  return waves_of(pieces) == 1 ? (groups + 3) / 4 : groups;
 }
 uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
 
@@ -441,40 +466,46 @@ hipError_t launch_norm(int dtype, const NormParams& p, hipStream_t st) {
   }
 }
 
-template <int DT, bool AFTER, bool WITH_B, int W, int NV>
+template <int DT, int MODE, bool WITH_B, int W, int NV>
 hipError_t norm_grad_as(const NormGradParams& p, hipStream_t st) {
-  hipLaunchKernelGGL((k_norm_grad<DT, W, NV, AFTER, WITH_B, (W <= 8)>), dim3((unsigned)((p.groups + rows_of<W>() - 1) / rows_of<W>())),
+  hipLaunchKernelGGL((k_norm_grad<DT, W, NV, MODE, WITH_B, (W <= 8)>), dim3((unsigned)workgroups_of(p.T, pieces_of(p.row_bytes))),
                      dim3(threads_of<W>()), 0, st, p);
   return hipGetLastError();
 }
-template <int DT, bool AFTER, bool WITH_B>
+template <int DT, int MODE, bool WITH_B>
 hipError_t norm_grad_b(const NormGradParams& p, hipStream_t st) {
   const uint32_t n = pieces_of(p.row_bytes);
-  if (n <= 64) return norm_grad_as<DT, AFTER, WITH_B, 1, 1>(p, st);
-  if (n <= 128) return norm_grad_as<DT, AFTER, WITH_B, 1, 2>(p, st);
-  if (n <= 256) return norm_grad_as<DT, AFTER, WITH_B, 1, 4>(p, st);
-  if (n <= 512) return norm_grad_as<DT, AFTER, WITH_B, 4, 2>(p, st);
-  if (n <= 1024) return norm_grad_as<DT, AFTER, WITH_B, 8, 2>(p, st);
-  if (n <= 2048) return norm_grad_as<DT, AFTER, WITH_B, 16, 2>(p, st);
-  if constexpr (DT == MOE_FP32) return norm_grad_as<DT, AFTER, WITH_B, 16, 4>(p, st);
+  if (n <= 64) return norm_grad_as<DT, MODE, WITH_B, 1, 1>(p, st);
+  if (n <= 128) return norm_grad_as<DT, MODE, WITH_B, 1, 2>(p, st);
+  if (n <= 256) return norm_grad_as<DT, MODE, WITH_B, 4, 1>(p, st);
+  if (n <= 512) return norm_grad_as<DT, MODE, WITH_B, 4, 2>(p, st);
+  if (n <= 1024) return norm_grad_as<DT, MODE, WITH_B, 8, 2>(p, st);
+  if (n <= 2048) return norm_grad_as<DT, MODE, WITH_B, 16, 2>(p, st);
+  if constexpr (DT == MOE_FP32) return norm_grad_as<DT, MODE, WITH_B, 16, 4>(p, st);
   return hipErrorInvalidValue;   // (no row of two-byte elements is that long)
 }
-template <int DT, bool AFTER>
-hipError_t norm_grad_type(const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
+template <int DT>
+hipError_t norm_grad_type(int mode, const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
   if (p.groups > 0) {
-    const hipError_t e = p.part_b != nullptr ? norm_grad_b<DT, AFTER, true>(p, st) : norm_grad_b<DT, AFTER, false>(p, st);
+    const bool b = p.part_b != nullptr;
+    hipError_t e;
+    switch (mode) {
+      case GRAD_BEFORE: e = b ? norm_grad_b<DT, GRAD_BEFORE, true>(p, st) : norm_grad_b<DT, GRAD_BEFORE, false>(p, st); break;
+      case GRAD_AFTER: e = b ? norm_grad_b<DT, GRAD_AFTER, true>(p, st) : norm_grad_b<DT, GRAD_AFTER, false>(p, st); break;
+      case GRAD_AFTER_TOKEN: e = b ? norm_grad_b<DT, GRAD_AFTER_TOKEN, true>(p, st) : norm_grad_b<DT, GRAD_AFTER_TOKEN, false>(p, st); break;
+      default: e = b ? norm_grad_b<DT, GRAD_AFTER_FULL, true>(p, st) : norm_grad_b<DT, GRAD_AFTER_FULL, false>(p, st); break;
+    }
     if (e != hipSuccess) return e;
   }
   if (!cp.grad_gamma && !cp.grad_beta && !cp.grad_gate) return hipSuccess;
   hipLaunchKernelGGL(k_norm_columns<DT>, dim3((unsigned)((cp.H + 31) / 32)), dim3(1024), 0, st, cp);
   return hipGetLastError();
 }
-template <bool AFTER>
-hipError_t launch_norm_grad(int dtype, const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
+hipError_t launch_norm_grad(int dtype, int mode, const NormGradParams& p, const NormColumnParams& cp, hipStream_t st) {
   switch (dtype) {
-    case MOE_BF16: return norm_grad_type<MOE_BF16, AFTER>(p, cp, st);
-    case MOE_FP16: return norm_grad_type<MOE_FP16, AFTER>(p, cp, st);
-    default: return norm_grad_type<MOE_FP32, AFTER>(p, cp, st);
+    case MOE_BF16: return norm_grad_type<MOE_BF16>(mode, p, cp, st);
+    case MOE_FP16: return norm_grad_type<MOE_FP16>(mode, p, cp, st);
+    default: return norm_grad_type<MOE_FP32>(mode, p, cp, st);
   }
 }
 
@@ -565,9 +596,9 @@ int moe_norm_after(const void* residual, const void* y, const void* gamma, const
 
 size_t moe_norm_workspace_bytes(int32_t T, int32_t H) {
   if (norm_shape(T, H) != MOE_OK) return 0;
-  const int groups2 = groups_of(T, pieces_of((uint32_t)H * 2)), groups4 = groups_of(T, pieces_of((uint32_t)H * 4));
-  const size_t groups = groups2 > groups4 ? groups2 : groups4;
-  return 2 * (groups > 0 ? groups : 1) * (size_t)H * 4;
+  const int two = workgroups_of(T, pieces_of((uint32_t)H * 2)), four = workgroups_of(T, pieces_of((uint32_t)H * 4));
+  const size_t rows = two > four ? two : four;
+  return 2 * (rows > 0 ? rows : 1) * (size_t)H * 4;
 }
 
 int moe_norm_before_backward(const void* sum, const void* gamma, const void* grad_x, const void* grad_sum, float residual_scale,
@@ -598,7 +629,7 @@ int moe_norm_before_backward(const void* sum, const void* gamma, const void* gra
   p.row_bytes = (uint32_t)row_bytes;
   p.groups = groups_of(T, pieces_of(p.row_bytes));
   p.part_a = columns ? (float*)workspace : nullptr;
-  p.part_b = grad_beta ? p.part_a + (size_t)p.groups * H : nullptr;
+  p.part_b = grad_beta ? p.part_a + (size_t)workgroups_of(T, pieces_of(p.row_bytes)) * H : nullptr;
   p.scale = residual_scale;
   p.eps = eps;
   p.inv_h = 1.0f / (float)H;
@@ -608,9 +639,9 @@ int moe_norm_before_backward(const void* sum, const void* gamma, const void* gra
   cp.gamma = p.gamma;
   cp.grad_gamma = grad_gamma;
   cp.grad_beta = grad_beta;
-  cp.groups = p.groups;
+  cp.groups = workgroups_of(T, pieces_of(p.row_bytes));
   cp.H = H;
-  return status_of(launch_norm_grad<false>(dtype, p, cp, (hipStream_t)hip_stream));
+  return status_of(launch_norm_grad(dtype, GRAD_BEFORE, p, cp, (hipStream_t)hip_stream));
 }
 
 int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, const void* gate, int32_t gate_kind,
@@ -647,7 +678,7 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   p.row_bytes = (uint32_t)row_bytes;
   p.groups = groups_of(T, pieces_of(p.row_bytes));
   p.part_a = columns ? (float*)workspace : nullptr;
-  p.part_b = grad_beta || (channel && grad_gate && beta) ? p.part_a + (size_t)p.groups * H : nullptr;
+  p.part_b = grad_beta || (channel && grad_gate && beta) ? p.part_a + (size_t)workgroups_of(T, pieces_of(p.row_bytes)) * H : nullptr;
   p.scale = residual_scale;
   p.eps = eps;
   p.inv_h = 1.0f / (float)H;
@@ -660,9 +691,10 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   cp.grad_gamma = grad_gamma;
   cp.grad_beta = grad_beta;
   cp.grad_gate = channel ? (float*)grad_gate : nullptr;
-  cp.groups = p.groups;
+  cp.groups = workgroups_of(T, pieces_of(p.row_bytes));
   cp.H = H;
-  return status_of(launch_norm_grad<true>(dtype, p, cp, (hipStream_t)hip_stream));
+  const int mode = full ? GRAD_AFTER_FULL : gate_kind == MOE_GATE_TOKEN ? GRAD_AFTER_TOKEN : GRAD_AFTER;
+  return status_of(launch_norm_grad(dtype, mode, p, cp, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"
