@@ -9,7 +9,6 @@
 namespace moe {
 
 constexpr int kSortChunk = 1024;        // pairs of a workgroup
-constexpr int kSortSmall = 4096;        // pairs up to which one workgroup does it all
 constexpr int kBuckets = kMaxExperts + 1;   // the last one, number E, takes the pairs without an expert
 constexpr int kMaxGateTopK = 64;
 constexpr int kMinRowColumns = 8, kMaxRowColumns = 65536;
@@ -57,54 +56,6 @@ __device__ __forceinline__ void scan_buckets(const int32_t* count, int32_t* firs
   }
 }
 
-// One workgroup for up to RUNS * 64 pairs: runs of 64 pairs, ranks inside a run by ballots, then prefix sums over the runs.
-template <int RUNS>
-__global__ __launch_bounds__(1024) void k_sort_small(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ offsets,
-                                                     int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
-  constexpr int kEach = (RUNS + 15) / 16;
-  __shared__ uint16_t run_cnt[RUNS][kBuckets];
-  __shared__ int32_t count[kBuckets], first[kBuckets];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int key[kEach], rank[kEach];
-#pragma unroll
-  for (int s = 0; s < kEach; s++) {
-    const int q = (wave * kEach + s) * 64 + lane;
-    key[s] = q < R ? bucket_of(ids, q, E) : -1;
-  }
-  for (int i = threadIdx.x; i < RUNS * kBuckets; i += blockDim.x) (&run_cnt[0][0])[i] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int s = 0; s < kEach; s++) {
-    const int run = wave * kEach + s;
-    const uint64_t same = same_bucket(key[s], key[s] >= 0), below = same & ((1ull << lane) - 1ull);
-    rank[s] = __popcll(below);
-    if (key[s] >= 0 && below == 0) run_cnt[run][key[s]] = (uint16_t)__popcll(same);
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < kBuckets; e += blockDim.x) {
-    int acc = 0;
-#pragma unroll
-    for (int r = 0; r < RUNS; r++) {
-      const int c = run_cnt[r][e];
-      run_cnt[r][e] = (uint16_t)acc;
-      acc += c;
-    }
-    count[e] = acc;
-  }
-  __syncthreads();
-  scan_buckets(count, first);
-  __syncthreads();
-#pragma unroll
-  for (int s = 0; s < kEach; s++) {
-    const int run = wave * kEach + s, q = run * 64 + lane, e = key[s];
-    if (e < 0) continue;
-    const int pos = first[e] + run_cnt[run][e] + rank[s];
-    perm[pos] = e < E ? q : -1;
-    inv[q] = e < E ? pos : -1;
-  }
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) offsets[e] = first[e];
-}
-
 // Pairs of each bucket in each chunk.
 __global__ __launch_bounds__(1024) void k_sort_hist(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ hist) {
   __shared__ int32_t count[kBuckets];
@@ -146,24 +97,48 @@ __global__ __launch_bounds__(1024) void k_sort_scan(int32_t* __restrict__ hist, 
   if (threadIdx.x == 0) total[e] = at;
 }
 
-// Stable scatter of a chunk.  total == nullptr: hist holds counts, and the workgroup sums those of the other chunks itself
-// (a thread per bucket and part of the chunks); otherwise hist holds the prefix sums.
+// Stable scatter of a chunk: a pair's row is the first one of its bucket, plus the bucket's pairs in the chunks before, in the runs of
+// 64 before, and in the lanes before.  Where the bucket's pairs in other chunks come from:
+// OWN: the workgroup counts all pairs itself, in 8 copies (by lane) of the counters, so that lanes with the same bucket seldom meet;
+// otherwise from hist, as prefix sums over the chunks with their total, or as counts (total == nullptr), summed here by a thread per
+// bucket and part of the chunks.
+template <bool OWN>
 __global__ __launch_bounds__(1024) void k_sort_scatter(const int32_t* __restrict__ ids, int R, int E, const int32_t* __restrict__ hist,
                                                        int n_chunks, const int32_t* __restrict__ total, int32_t* __restrict__ offsets,
                                                        int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
-  constexpr int kRuns = kSortChunk / 64;
+  constexpr int kRuns = kSortChunk / 64, kCopies = 8;
   __shared__ int32_t run_cnt[kRuns][kBuckets];
   __shared__ int32_t count[kBuckets], first[kBuckets], before[kBuckets];
+  __shared__ int32_t own[OWN ? 2 : 1][OWN ? kCopies : 1][OWN ? kBuckets : 1];   // pairs of earlier chunks, and of this and later ones
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = E + 1;
   const int q = blockIdx.x * kSortChunk + threadIdx.x;
   const int e = q < R ? bucket_of(ids, q, E) : -1;
   for (int i = threadIdx.x; i < kRuns * kBuckets; i += 1024) (&run_cnt[0][0])[i] = 0;
+  if constexpr (OWN)
+    for (int i = threadIdx.x; i < 2 * kCopies * kBuckets; i += 1024) (&own[0][0][0])[i] = 0;
   for (int i = threadIdx.x; i < kBuckets; i += 1024) {
-    count[i] = total != nullptr && i < n ? total[i] : 0;
-    before[i] = total != nullptr && i < n ? hist[(size_t)blockIdx.x * n + i] : 0;
+    count[i] = !OWN && total != nullptr && i < n ? total[i] : 0;
+    before[i] = !OWN && total != nullptr && i < n ? hist[(size_t)blockIdx.x * n + i] : 0;
   }
   __syncthreads();
-  if (total == nullptr) {
+  if constexpr (OWN) {
+    if (n_chunks > 1) {
+      const int copy = lane & (kCopies - 1), fours = R / 4;
+      auto one = [&](int id, int later) { atomicAdd(&own[later][copy][(unsigned)id < (unsigned)E ? id : E], 1); };
+#pragma unroll 4
+      for (int i = threadIdx.x; i < fours; i += 1024) {
+        const int4 v = ((const int4*)ids)[i];
+        const int later = i * 4 >= (int)blockIdx.x * kSortChunk;   // (four pairs never lie in two chunks)
+        one(v.x, later);
+        one(v.y, later);
+        one(v.z, later);
+        one(v.w, later);
+      }
+      if (fours * 4 + (int)threadIdx.x < R) one(ids[fours * 4 + threadIdx.x], 1);   // up to three, in the last chunk
+    } else if (e >= 0) {
+      atomicAdd(&own[1][lane & (kCopies - 1)][e], 1);
+    }
+  } else if (total == nullptr) {
     const int parts = n <= 1024 / 16 ? 16 : n <= 1024 / 8 ? 8 : 3;
     const int b = threadIdx.x % n, part = threadIdx.x / n;
     if (part < parts) {
@@ -182,6 +157,19 @@ __global__ __launch_bounds__(1024) void k_sort_scatter(const int32_t* __restrict
   const int rank = __popcll(below);
   if (e >= 0 && below == 0) run_cnt[wave][e] = __popcll(same);
   __syncthreads();
+  if constexpr (OWN) {
+    for (int i = threadIdx.x; i < n; i += 1024) {
+      int b = 0, a = 0;
+#pragma unroll
+      for (int c = 0; c < kCopies; c++) {
+        b += own[0][c][i];
+        a += own[1][c][i];
+      }
+      before[i] = b;
+      count[i] = a + b;
+    }
+    __syncthreads();
+  }
   scan_buckets(count, first);
   for (int i = threadIdx.x - 64; i >= 0 && i < n; i += 1024 - 64) {   // (the first wavefront is scanning)
     int acc = before[i];
@@ -248,7 +236,7 @@ __global__ __launch_bounds__(256) void k_dispatch(const char* x, const int32_t* 
       if ((unsigned)pos[j] >= (unsigned)R) continue;   // no row
       char* dst = rows + (size_t)pos[j] * row_bytes;
 #pragma unroll
-      for (int i = 0; i < NV; i++) store_piece(dst, start + i * (LP * 16), row_bytes, v[i]);
+      for (int i = 0; i < NV; i++) store_once(dst, start + i * (LP * 16), row_bytes, v[i]);
     }
   }
 }
@@ -282,7 +270,7 @@ __global__ __launch_bounds__(256) void k_combine_rows(const char* rows, const in
     for (int j = 0; j < KK; j++)
       if ((unsigned)pos[j] < (unsigned)R)
 #pragma unroll
-        for (int i = 0; i < NV; i++) v[j][i] = load_piece(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
+        for (int i = 0; i < NV; i++) v[j][i] = load_once(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
 #pragma unroll
     for (int j = 0; j < KK; j++)
       if ((unsigned)pos[j] < (unsigned)R)
@@ -329,13 +317,13 @@ __global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char*
       const uint32_t start = base + at.lane * 16;
       u32x4 gv[NV], rv[KK][NV];
 #pragma unroll
-      for (int i = 0; i < NV; i++) gv[i] = load_piece(src, start + i * (LP * 16), row_bytes);
+      for (int i = 0; i < NV; i++) gv[i] = load_once(src, start + i * (LP * 16), row_bytes);
       if (rows != nullptr) {
 #pragma unroll
         for (int j = 0; j < KK; j++)
           if ((unsigned)pos[j] < (unsigned)R)
 #pragma unroll
-            for (int i = 0; i < NV; i++) rv[j][i] = load_piece(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
+            for (int i = 0; i < NV; i++) rv[j][i] = load_once(rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes);
       }
 #pragma unroll
       for (int i = 0; i < NV; i++) {
@@ -359,7 +347,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char*
           float o[N];
 #pragma unroll
           for (int c = 0; c < N; c++) o[c] = wj[j] * gf[c];
-          store_piece(grad_rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes, V::pack(o));
+          store_once(grad_rows + (size_t)pos[j] * row_bytes, start + i * (LP * 16), row_bytes, V::pack(o));
         }
       }
     }
@@ -388,26 +376,58 @@ __global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char*
 }
 
 // The weights of a token are the softmax of its kept logits, so d w_i / d logit_j = w_i (delta_ij - w_j) among them:
-// grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A thread takes 4 experts of a token.
+// grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A thread takes 4 experts of a token and reads its
+// slots in groups of K, all of a group at once.
+template <int K>
 __global__ __launch_bounds__(256) void k_route_topk_grad(const int32_t* __restrict__ ids, const float* __restrict__ w,
                                                          const float* __restrict__ gw, int64_t n_units, int E, int k, int quads,
                                                          float* __restrict__ out) {
   const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (unit >= n_units) return;
-  const int64_t t = unit / quads;
-  const int e0 = (int)(unit - t * quads) * 4;
-  float sum = 0.f;
-  for (int j = 0; j < k; j++) sum = fmaf(gw[t * k + j], w[t * k + j], sum);
+  const int t = (int)((uint32_t)unit / (uint32_t)quads);
+  const int e0 = ((int)unit - t * quads) * 4;
+  const size_t first = (size_t)t * k;
   float o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < k; j++) {
-    const int e = ids[t * k + j] - e0;
-    const float d = w[t * k + j] * (gw[t * k + j] - sum);
+  int id[K];
+  float wj[K], gj[K], sum = 0.f;
+  auto read = [&](int j0) {
 #pragma unroll
-    for (int c = 0; c < 4; c++) o[c] += e == c ? d : 0.f;
+    for (int j = 0; j < K; j++) {
+      const bool there = j0 + j < k;
+      id[j] = there ? ids[first + j0 + j] - e0 : -1;
+      wj[j] = there ? w[first + j0 + j] : 0.f;
+      gj[j] = there ? gw[first + j0 + j] : 0.f;
+    }
+  };
+  auto add = [&]() {
+#pragma unroll
+    for (int j = 0; j < K; j++) {
+      const float d = wj[j] * (gj[j] - sum);
+#pragma unroll
+      for (int c = 0; c < 4; c++) o[c] += id[j] == c ? d : 0.f;
+    }
+  };
+  for (int j0 = 0; j0 < k; j0 += K) {
+    read(j0);
+#pragma unroll
+    for (int j = 0; j < K; j++) sum = fmaf(gj[j], wj[j], sum);
   }
+  if (k <= K) {
+    add();
+  } else {
+    for (int j0 = 0; j0 < k; j0 += K) {
+      read(j0);
+      add();
+    }
+  }
+  float* dst = out + (size_t)t * E + e0;
+  if (E % 4 == 0) {
+    *(float4*)dst = make_float4(o[0], o[1], o[2], o[3]);
+  } else {
 #pragma unroll
-  for (int c = 0; c < 4; c++)
-    if (e0 + c < E) out[t * E + e0 + c] = o[c];
+    for (int c = 0; c < 4; c++)
+      if (e0 + c < E) dst[c] = o[c];
+  }
 }
 
 namespace {
@@ -505,7 +525,12 @@ hipError_t combine_grad_type(const RowCall& c, const void* g, const void* rows, 
 }
 
 int n_chunks_of(int64_t R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
-constexpr int kSortOwnSums = 512;   // chunks up to which the scatter sums the counts itself
+// Where a chunk's workgroup has the counts of the others from.  us, it counts all pairs itself / counts by a launch of their own:
+// 16384 pairs of 64 experts 5.4 / 6.8, 32768 6.5 / 7.2, 65536 8.7 / 7.1, of 8 experts 12.4 / 6.7; a launch also takes 2.6 us of the host.
+constexpr int kSortOwnCounts = 32;
+// It sums the counts of the chunks itself while they are few: 256 chunks of 65 buckets 6.9, 512 of 257 28, against 3.4 and 9 for 1024 chunks
+// of 9 buckets with their prefix sums by a launch of their own.
+constexpr int kSortOwnSums = 32768;   // chunks x buckets
 
 // Checks that the row operators share; *c is set where there is something to do.
 int row_call(int32_t T, int32_t H, int32_t k, int32_t dtype, void* hip_stream, RowCall* c) {
@@ -555,17 +580,16 @@ int moe_sort_tokens(const int32_t* topk_ids, int32_t T, int32_t E, int32_t k, in
   if (!topk_ids || !perm || !inv_perm || !workspace) return MOE_ERR_INVALID_ARG;
   if (!aligned16(topk_ids) || !aligned16(perm) || !aligned16(inv_perm) || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
   if (workspace_bytes < moe_sort_workspace_bytes(T, E, k)) return MOE_ERR_WORKSPACE_TOO_SMALL;
-  if (R <= kSortSmall) {
-    if (R <= 1024) hipLaunchKernelGGL((k_sort_small<16>), dim3(1), dim3(1024), 0, st, topk_ids, R, E, expert_offsets, perm, inv_perm);
-    else hipLaunchKernelGGL((k_sort_small<kSortSmall / 64>), dim3(1), dim3(1024), 0, st, topk_ids, R, E, expert_offsets, perm, inv_perm);
-    return status_of(hipGetLastError());
-  }
   int32_t* hist = (int32_t*)workspace;
   const int n_chunks = n_chunks_of(R);
-  int32_t* total = n_chunks > kSortOwnSums ? hist + (size_t)n_chunks * (E + 1) : nullptr;
+  if (n_chunks <= kSortOwnCounts) {
+    hipLaunchKernelGGL(k_sort_scatter<true>, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, nullptr, n_chunks, nullptr, expert_offsets, perm, inv_perm);
+    return status_of(hipGetLastError());
+  }
+  int32_t* total = (int64_t)n_chunks * (E + 1) > kSortOwnSums ? hist + (size_t)n_chunks * (E + 1) : nullptr;
   hipLaunchKernelGGL(k_sort_hist, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist);
   if (total) hipLaunchKernelGGL(k_sort_scan, dim3(E + 1), dim3(1024), 0, st, hist, n_chunks, E, total);
-  hipLaunchKernelGGL(k_sort_scatter, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist, n_chunks, total, expert_offsets, perm, inv_perm);
+  hipLaunchKernelGGL(k_sort_scatter<false>, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist, n_chunks, total, expert_offsets, perm, inv_perm);
   return status_of(hipGetLastError());
 }
 
@@ -626,8 +650,9 @@ int moe_route_topk_backward(const int32_t* topk_ids, const float* topk_weights, 
   if (!aligned16(topk_ids) || !aligned16(topk_weights) || !aligned16(grad_weights) || !aligned16(grad_logits)) return MOE_ERR_INVALID_ARG;
   const int quads = (E + 3) / 4;
   const int64_t n_units = (int64_t)T * quads;
-  hipLaunchKernelGGL(k_route_topk_grad, dim3((unsigned)((n_units + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, topk_ids, topk_weights,
-                     grad_weights, n_units, E, k, quads, grad_logits);
+  auto kernel = k <= 2 ? k_route_topk_grad<2> : k <= 4 ? k_route_topk_grad<4> : k_route_topk_grad<8>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((n_units + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, topk_ids, topk_weights, grad_weights,
+                     n_units, E, k, quads, grad_logits);
   return status_of(hipGetLastError());
 }
 
