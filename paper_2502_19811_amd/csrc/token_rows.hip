@@ -440,7 +440,8 @@ struct RowCall {
   size_t rows_bytes() const { return (size_t)R * row_bytes; }
 };
 
-// Lanes of a token.
+// Lanes of a token, as many as a row has pieces.  us for 32768 tokens of 64 columns, k = 2, with 8 lanes / 64: combine 3.9 / 8.6, its gradient
+// 5.9 / 11.6; of 256 columns with 32 / 64: 11.6 / 12.2, 16.7 / 18.3.
 int lanes_of(const RowCall& c) { return c.row_bytes <= 8 * 16 ? 8 : c.row_bytes <= 32 * 16 ? 32 : 64; }
 
 template <int LP, int NV>
@@ -477,7 +478,7 @@ hipError_t combine_k(const RowCall& c, const void* rows, const int32_t* inv, con
   switch (lanes_of(c)) {
     case 8: return combine_as<DT, K, 8, 1>(c, rows, inv, w, out);
     case 32: return combine_as<DT, K, 32, 1>(c, rows, inv, w, out);
-    default: return combine_as<DT, K, 64, (K == 8 || K == 4) ? 2 : 4>(c, rows, inv, w, out);
+    default: return combine_as<DT, K, 64, 2>(c, rows, inv, w, out);   // 1 or 4 pieces a lane are up to 5 % slower at one size or another
   }
 }
 template <int DT>
@@ -503,16 +504,17 @@ hipError_t combine_grad_as(const RowCall& c, const void* g, const void* rows, co
                      (char*)grad_rows, grad_w, c.T, c.k, c.R, c.row_bytes);
   return hipGetLastError();
 }
-constexpr int kGradTokensPerWave = 4096;   // tokens from which a wavefront has one to itself
+// Four wavefronts take a token, so that its pieces are requested together.  us, one wavefront a token with 1 / 2 / 4 pieces a lane, four
+// with 1 / 2: 32768 tokens of 4096 columns, k = 2 284 / 287 / 268, 238 / 228; 16384 of 2048, k = 4 127 / 120 / 113, 102 / 110; 4096 of 3584, k = 8
+// 98 / 99 / 99, 93 / 92; 128 of 4096, k = 2 6.4 / 6.1 / 5.6, 3.5 / 3.5; 16384 of 600, k = 2 25 / 24 / 25, 23 / 28.
 template <int DT, int K>
 hipError_t combine_grad_k(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
-  constexpr int NV = K == 8 ? 1 : 2;
   switch (lanes_of(c)) {
     case 8: return combine_grad_as<DT, K, 8, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
     case 32: return combine_grad_as<DT, K, 32, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
     default:
-      if (c.T >= kGradTokensPerWave) return combine_grad_as<DT, K, 64, NV, 1>(c, g, rows, inv, w, grad_rows, grad_w);
-      return combine_grad_as<DT, K, 64, NV, 4>(c, g, rows, inv, w, grad_rows, grad_w);
+      if (c.row_bytes <= 4 * 1024) return combine_grad_as<DT, K, 64, 1, 4>(c, g, rows, inv, w, grad_rows, grad_w);
+      return combine_grad_as<DT, K, 64, 2, 4>(c, g, rows, inv, w, grad_rows, grad_w);
   }
 }
 template <int DT>

@@ -191,6 +191,32 @@ def test_captured_in_a_graph(T):
         print(f"  replay {rep} ok", flush=True)
 
 
+def test_two_graphs_with_the_same_workspaces():
+    """Scratch holds nothing between calls: graphs that share it may be replayed in any order, one after the other."""
+    a, b = Block(1500, 264, 16, 4, torch.bfloat16, 71, False), Block(900, 264, 16, 4, torch.bfloat16, 72, True)
+    b.sort_ws, b.norm_ws = a.sort_ws, a.norm_ws            # those of the larger batch
+    graphs, eager = [], []
+    for blk in (a, b):
+        blk.forward()
+        _without_products(blk)
+        torch.cuda.synchronize()
+        eager.append([v.clone() for v in _results(blk)])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            _without_products(blk)
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1):
+        blk = (a, b)[i]
+        for v in _results(blk):
+            v.zero_()
+        a.sort_ws.fill_(0xff)
+        a.norm_ws.fill_(0xff)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        for x, y in zip(_results(blk), eager[i]):
+            assert torch.equal(x, y)
+
+
 def test_on_another_stream():
     b = Block(900, 264, 8, 2, torch.bfloat16, 80, True)
     b.forward()

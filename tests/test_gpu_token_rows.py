@@ -1,5 +1,5 @@
 """Row order, dispatch, combine, their gradients and the gate's against definitions in 64 bits: sizes on both sides of every variant
-(one workgroup / many, chunks summed by the scatter / beforehand, 8 / 32 / 64 lanes a token, numbers of slots with and without a
+(one workgroup / many, pairs counted by every workgroup / by a launch of its own, the counts summed by the scatter / beforehand, 8 / 32 / 64 lanes a token, numbers of slots with and without a
 kernel of their own, rows of odd lengths), slots without an expert, and what lies where nothing may be read or written."""
 import numpy as np
 import pytest
@@ -20,7 +20,8 @@ def _sort(moe, ids, E):
 
 @pytest.mark.parametrize("T,E,k,dropped", [
     (1, 1, 1, 0.0), (1, 256, 64, 0.0), (3, 4, 2, 0.5), (16, 8, 2, 0.0), (31, 200, 33, 0.1), (512, 8, 2, 0.0), (513, 8, 2, 0.2), (2048, 64, 2, 0.0),
-    (2049, 64, 2, 0.3), (1000, 63, 8, 0.0), (1000, 64, 8, 0.1), (1000, 127, 8, 0.1), (1000, 128, 8, 0.0), (5000, 256, 8, 0.1),
+    (2049, 64, 2, 0.3), (1000, 63, 8, 0.0), (1000, 64, 8, 0.1), (1000, 127, 8, 0.1), (1000, 128, 8, 0.0), (4096, 16, 8, 0.1), (4097, 16, 8, 0.1), (8000, 100, 8, 0.1),
+    (5000, 256, 8, 0.1),
     (65536, 8, 8, 0.05), (70001, 8, 8, 0.05), (262144 + 77, 256, 8, 0.01)])
 def test_row_order(T, E, k, dropped):
     import paper_2502_19811_amd as moe
@@ -219,6 +220,19 @@ def test_indices_outside_are_no_row(dtype):
     moe.moe_combine(rows, inv, None, a)
     moe.moe_combine(rows, clean, None, b)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ro.DTYPES, ids=str)
+def test_no_tokens(dtype):
+    import paper_2502_19811_amd as moe
+    x, rows, inv = (torch.empty(s, dtype=d, device="cuda") for s, d in (((0, 64), dtype), ((0, 64), dtype), ((0, 2), torch.int32)))
+    w, logits = torch.empty((0, 2), device="cuda"), torch.empty((0, 4), device="cuda")
+    moe.moe_dispatch(x, inv, rows)
+    moe.moe_dispatch_backward(rows, inv, x)
+    moe.moe_combine(rows, inv, w, x)
+    moe.moe_combine_backward(x, rows, inv, w, rows, w)
+    moe.moe_route_topk_backward(inv, w, w, logits)
+    torch.cuda.synchronize()
 
 
 def test_rows_beyond_4_gib():
