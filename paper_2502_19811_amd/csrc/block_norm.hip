@@ -6,6 +6,9 @@
 // through LDS.  The mean of a "layer" norm is taken off before the squares are summed.
 #include "row_vector.h"
 
+// Fused operations are written out, and no others made: a result does not depend on which variant computes it.
+#pragma clang fp contract(off)
+
 namespace moe {
 
 constexpr int kMinNormColumns = 8, kMaxNormColumns = 16384;
@@ -69,27 +72,55 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int which, bool ragged) 
 template <int W> constexpr int threads_of() { return W > 4 ? W * 64 : 256; }
 template <int W> constexpr int rows_of() { return W > 4 ? 1 : 4 / W; }   // rows of a workgroup
 
-// Runs body(piece, column, counts) over a lane's elements; counts is false for those that are another lane's, too, or nobody's.
-template <int NV, int N, int UNIT, typename F>
-__device__ __forceinline__ void each_counted(const uint32_t (&at)[NV], uint32_t row_bytes, bool exact, F body) {
-  if (exact) {
+// A lane's pieces of a row.  EXACT: the row has W * NV * 64 of them, one for everybody.  Otherwise it has more than half as many (and with one
+// wavefront and at most two pieces a lane more than the last piece's beginning): the later pieces may lie behind its end, for some wavefronts.
+// Whether a wavefront has any of a piece, and all of it, is the same in its lanes: what is not there is neither loaded nor computed
+// (8192 rows of 4104 columns, eight wavefronts with two pieces a lane, behind the block: 49 us with all of them, 41 without).
+template <int DT, int W, int NV, bool EXACT>
+struct Pieces {
+  static constexpr int N = Row<DT>::kVec;
+  uint32_t at[NV], first, row_bytes;
+  __device__ __forceinline__ Pieces(int wave, int lane, uint32_t bytes) : first((uint32_t)(wave % W) * 1024), row_bytes(bytes) {
+#pragma unroll
+    for (int i = 0; i < NV; i++) at[i] = (uint32_t)(i * W * 1024) + first + lane * 16;
+  }
+  __device__ __forceinline__ bool any(int i) const { return EXACT || i < NV / 2 || (W == 1 && NV <= 2) || (uint32_t)(i * W * 1024) + first < row_bytes; }
+  __device__ __forceinline__ bool all(int i) const { return EXACT || i < NV / 2 || (uint32_t)((i * W + 1) * 1024) + first <= row_bytes; }
+  __device__ __forceinline__ void store(char* row, int i, const u32x4& v) const {
+    if constexpr (EXACT) *(u32x4*)(row + at[i]) = v;
+    else store_piece(row, at[i], row_bytes, v);
+  }
+  __device__ __forceinline__ void store_rarely_read(char* row, int i, const u32x4& v) const {
+    if constexpr (EXACT) __builtin_nontemporal_store(v, (u32x4*)(row + at[i]));
+    else store_once(row, at[i], row_bytes, v);
+  }
+  // body(piece) for the pieces that are there
+  template <typename F>
+  __device__ __forceinline__ void each(F body) const {
 #pragma unroll
     for (int i = 0; i < NV; i++)
-#pragma unroll
-      for (int c = 0; c < N; c++) body(i, c, true);
-  } else {
+      if (any(i)) body(i);
+  }
+  // body(piece, column, counts) for their elements; counts is false for those that another lane has, too
+  template <typename F>
+  __device__ __forceinline__ void each_element(F body) const {
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      const int from = counted<UNIT>(at[i], row_bytes);
+      if (all(i)) {
 #pragma unroll
-      for (int c = 0; c < N; c++) body(i, c, c >= from);
+        for (int c = 0; c < N; c++) body(i, c, true);
+      } else if (any(i)) {
+        const int from = counted<Row<DT>::kBytes>(at[i], row_bytes);
+#pragma unroll
+        for (int c = 0; c < N; c++) body(i, c, c >= from);
+      }
     }
   }
-}
+};
 
 // n = v * r - mean * r, one fused operation an element whatever the norm: at 16 lanes a cycle and SIMD an operation on every element of
 // 16384 x 4096 takes 1.7 us, so the gradients, which read three rows, have room for about 30.
-template <int DT, int W, int NV, bool AFTER>
+template <int DT, int W, int NV, bool AFTER, bool EXACT>
 __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   using V = Row<DT>;
   constexpr int N = V::kVec;
@@ -97,33 +128,28 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   const int t = blockIdx.x * rows_of<W>() + wave / W;
   if (t >= p.T) return;   // (W > 1: the whole workgroup or nobody)
   const size_t row = (size_t)t * p.row_bytes;
-  const bool exact = p.row_bytes == W * NV * 1024, ragged = p.row_bytes % 16 != 0;
-  uint32_t at[NV];
-#pragma unroll
-  for (int i = 0; i < NV; i++) at[i] = (uint32_t)((i * W + wave % W) * 64 + lane) * 16;
+  const bool ragged = !EXACT && p.row_bytes % 16 != 0;
+  const Pieces<DT, W, NV, EXACT> mine(wave, lane, p.row_bytes);
   u32x4 rv[NV], bv[NV], gv[NV], hv[NV];
   if (!AFTER || p.residual != nullptr)
-#pragma unroll
-    for (int i = 0; i < NV; i++) rv[i] = load_once(p.residual + row, at[i], p.row_bytes);
+    mine.each([&](int i) { rv[i] = load_once(p.residual + row, mine.at[i], p.row_bytes); });
   if (AFTER || p.branch != nullptr)
-#pragma unroll
-    for (int i = 0; i < NV; i++) bv[i] = load_once(p.branch + row, at[i], p.row_bytes);
+    mine.each([&](int i) { bv[i] = load_once(p.branch + row, mine.at[i], p.row_bytes); });
   float scale = p.scale;
   const bool gated = AFTER && (p.gate_kind == MOE_GATE_CHANNEL || p.gate_kind == MOE_GATE_FULL);
   if constexpr (AFTER) {
     if (gated) {
       const char* gate = p.gate + (p.gate_kind == MOE_GATE_FULL ? row : 0);
-#pragma unroll
-      for (int i = 0; i < NV; i++) hv[i] = load_piece(gate, at[i], p.row_bytes);
+      mine.each([&](int i) { hv[i] = load_piece(gate, mine.at[i], p.row_bytes); });
     } else if (p.gate_kind == MOE_GATE_TOKEN) {
       scale *= ((const float*)p.gate)[t];
     }
   }
-#pragma unroll
-  for (int i = 0; i < NV; i++) gv[i] = load_piece(p.gamma, at[i], p.row_bytes);
+  mine.each([&](int i) { gv[i] = load_piece(p.gamma, mine.at[i], p.row_bytes); });
   float v[NV][N];
 #pragma unroll
   for (int i = 0; i < NV; i++) {
+    if (!mine.any(i)) continue;
     if constexpr (AFTER) {
       V::unpack(bv[i], v[i]);
     } else {
@@ -139,15 +165,15 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   float mean = 0.f, sq[1] = {0.f};
   if (p.layer) {
     float s[1] = {0.f};
-    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) { s[0] += counts ? v[i][c] : 0.f; });
+    mine.each_element([&](int i, int c, bool counts) { s[0] += counts ? v[i][c] : 0.f; });
     row_sums<W>(s, 0, false);
     mean = s[0] * p.inv_h;
-    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+    mine.each_element([&](int i, int c, bool counts) {
       const float d = counts ? v[i][c] - mean : 0.f;
       sq[0] = fmaf(d, d, sq[0]);
     });
   } else {
-    each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+    mine.each_element([&](int i, int c, bool counts) {
       const float d = counts ? v[i][c] : 0.f;
       sq[0] = fmaf(d, d, sq[0]);
     });
@@ -156,16 +182,16 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   const float r = 1.f / sqrtf(fmaf(sq[0], p.inv_h, p.eps)), minus = p.layer ? -mean * r : 0.f;
   if constexpr (!AFTER)
     if (p.sum != nullptr)
-#pragma unroll
-      for (int i = 0; i < NV; i++) store_once(p.sum + row, at[i], p.row_bytes, V::pack(v[i]));
+      mine.each([&](int i) { mine.store_rarely_read(p.sum + row, i, V::pack(v[i])); });
 #pragma unroll
   for (int i = 0; i < NV; i++) {
+    if (!mine.any(i)) continue;
     float o[N], f[N];
     V::unpack(gv[i], f);
 #pragma unroll
     for (int c = 0; c < N; c++) o[c] = fmaf(v[i][c], r, minus) * f[c];
     if (p.beta != nullptr) {
-      V::unpack(load_piece(p.beta, at[i], p.row_bytes), f);
+      V::unpack(load_piece(p.beta, mine.at[i], p.row_bytes), f);
 #pragma unroll
       for (int c = 0; c < N; c++) o[c] += f[c];
     }
@@ -181,7 +207,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
 #pragma unroll
       for (int c = 0; c < N; c++) o[c] = fmaf(scale, o[c], f[c]);
     }
-    store_piece(p.out + row, at[i], p.row_bytes, V::pack(o));
+    mine.store(p.out + row, i, V::pack(o));
   }
 }
 
@@ -191,33 +217,33 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
 // A group of W wavefronts takes rows group, group + groups, ... and keeps, in registers, its columns' sums over them: A of
 // f * n and B of f, f the gradient of gamma * n + beta but for the scale and a channel gate, which are factors of the sums; they go
 // to part_a and part_b, a row for each workgroup, which k_norm_columns adds up in a fixed order.  The next row is requested before the present one
-// is summed up (PRE), which the largest rows have no registers for.
+// is summed up (PRE), which the largest rows have no registers for.  Its loads are waited for by counting what was requested after them,
+// which takes that nothing is conditional: ALL says that the row is exact and that every optional row is given.
 enum { GRAD_BEFORE = 0, GRAD_AFTER = 1, GRAD_AFTER_TOKEN = 2, GRAD_AFTER_FULL = 3 };   // AFTER: no gate or a channel gate
-template <int DT, int W, int NV, int MODE, bool WITH_B, bool PRE>
+template <int DT, int W, int NV, int MODE, bool WITH_B, bool PRE, bool ALL>
 __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p) {
   using V = Row<DT>;
   constexpr int N = V::kVec;
   constexpr bool kToken = MODE == GRAD_AFTER_TOKEN, kFull = MODE == GRAD_AFTER_FULL;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int group = blockIdx.x * rows_of<W>() + wave / W;
-  const bool exact = p.row_bytes == W * NV * 1024, ragged = p.row_bytes % 16 != 0;
-  uint32_t at[NV];
-#pragma unroll
-  for (int i = 0; i < NV; i++) at[i] = (uint32_t)((i * W + wave % W) * 64 + lane) * 16;
+  const bool ragged = !ALL && p.row_bytes % 16 != 0;
+  const Pieces<DT, W, NV, ALL> mine(wave, lane, p.row_bytes);
   float gamma[NV][N];   // with a channel gate multiplied in
   u32x4 beta[NV];
   const bool has_beta = (kToken || kFull) && p.beta != nullptr;
 #pragma unroll
   for (int i = 0; i < NV; i++) {
-    V::unpack(load_piece(p.gamma, at[i], p.row_bytes), gamma[i]);
+    if (!mine.any(i)) continue;
+    V::unpack(load_piece(p.gamma, mine.at[i], p.row_bytes), gamma[i]);
     if constexpr (MODE == GRAD_AFTER)
       if (p.gate_kind == MOE_GATE_CHANNEL) {
         float h[N];
-        V::unpack(load_piece(p.gate, at[i], p.row_bytes), h);
+        V::unpack(load_piece(p.gate, mine.at[i], p.row_bytes), h);
 #pragma unroll
         for (int c = 0; c < N; c++) gamma[i][c] *= h[c];
       }
-    if (has_beta) beta[i] = load_piece(p.beta, at[i], p.row_bytes);
+    if (has_beta) beta[i] = load_piece(p.beta, mine.at[i], p.row_bytes);
   }
   float acc_a[NV][N], acc_b[WITH_B ? NV : 1][N];
 #pragma unroll
@@ -230,13 +256,10 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
   u32x4 vv[NV], gg[NV], hh[kFull ? NV : 1];
   auto request = [&](int t) {
     const size_t row = (size_t)t * p.row_bytes;
-#pragma unroll
-    for (int i = 0; i < NV; i++) vv[i] = load_once(p.v + row, at[i], p.row_bytes);
-#pragma unroll
-    for (int i = 0; i < NV; i++) gg[i] = load_once(p.g + row, at[i], p.row_bytes);
+    mine.each([&](int i) { vv[i] = load_once(p.v + row, mine.at[i], p.row_bytes); });
+    mine.each([&](int i) { gg[i] = load_once(p.g + row, mine.at[i], p.row_bytes); });
     if constexpr (kFull)
-#pragma unroll
-      for (int i = 0; i < NV; i++) hh[i] = load_once(p.gate + row, at[i], p.row_bytes);
+      mine.each([&](int i) { hh[i] = load_once(p.gate + row, mine.at[i], p.row_bytes); });
   };
   int flip = 0;
   if constexpr (PRE)
@@ -246,12 +269,12 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
     if constexpr (!PRE) request(t);
     u32x4 more[NV];   // what the stream's gradient is before
     if constexpr (MODE == GRAD_BEFORE)
-      if (p.more != nullptr)
-#pragma unroll
-        for (int i = 0; i < NV; i++) more[i] = load_once(p.more + row, at[i], p.row_bytes);
+      if (ALL || p.more != nullptr)
+        mine.each([&](int i) { more[i] = load_once(p.more + row, mine.at[i], p.row_bytes); });
     float v[NV][N], f[NV][N], g[kFull ? NV : 1][N];   // f: gradient of gamma * n + beta, but for the factors said above
 #pragma unroll
     for (int i = 0; i < NV; i++) {
+      if (!mine.any(i)) continue;
       V::unpack(vv[i], v[i]);
       V::unpack(gg[i], f[i]);
       if constexpr (kFull) {
@@ -271,20 +294,20 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
     float s[3] = {0.f, 0.f, 0.f};   // sums of the squares, of e * (v - mean), of f * beta
     if (p.layer) {
       float m[2] = {0.f, 0.f};
-      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+      mine.each_element([&](int i, int c, bool counts) {
         m[0] += counts ? v[i][c] : 0.f;
-        m[1] += counts ? f[i][c] * gamma[i][c] : 0.f;
+        m[1] = fmaf(counts ? f[i][c] : 0.f, counts ? gamma[i][c] : 0.f, m[1]);
       });
       row_sums<W>(m, flip, false);
       mean = m[0] * p.inv_h;
       sum_e = m[1];
-      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+      mine.each_element([&](int i, int c, bool counts) {
         const float d = counts ? v[i][c] - mean : 0.f;
         s[0] = fmaf(d, d, s[0]);
         s[1] = fmaf(counts ? f[i][c] * gamma[i][c] : 0.f, d, s[1]);
       });
     } else {
-      each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) {
+      mine.each_element([&](int i, int c, bool counts) {
         const float d = counts ? v[i][c] : 0.f;
         s[0] = fmaf(d, d, s[0]);
         s[1] = fmaf(counts ? f[i][c] * gamma[i][c] : 0.f, d, s[1]);
@@ -295,7 +318,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
         float b[NV][N];
 #pragma unroll
         for (int i = 0; i < NV; i++) V::unpack(beta[i], b[i]);
-        each_counted<NV, N, V::kBytes>(at, p.row_bytes, exact, [&](int i, int c, bool counts) { s[2] += counts ? f[i][c] * b[i][c] : 0.f; });
+        mine.each_element([&](int i, int c, bool counts) { s[2] = fmaf(counts ? f[i][c] : 0.f, counts ? b[i][c] : 0.f, s[2]); });
       }
     row_sums<W>(s, flip, ragged);
     flip ^= 1;
@@ -309,11 +332,12 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
     const float rt = kToken ? r * gate_t : r, minus_t = kToken ? minus * gate_t : minus;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
+      if (!mine.any(i)) continue;
       float o[N], x[N];
       if constexpr (MODE == GRAD_BEFORE) {
 #pragma unroll
         for (int c = 0; c < N; c++) x[c] = 0.f;
-        if (p.more != nullptr) V::unpack(more[i], x);
+        if (ALL || p.more != nullptr) V::unpack(more[i], x);
       }
 #pragma unroll
       for (int c = 0; c < N; c++) {
@@ -322,22 +346,22 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
         o[c] = fmaf(c1, f[i][c] * gamma[i][c], fmaf(c2, v[i][c], c0));
         if constexpr (MODE == GRAD_BEFORE) o[c] += x[c];
       }
-      store_piece(p.grad_v + row, at[i], p.row_bytes, V::pack(o));
+      mine.store(p.grad_v + row, i, V::pack(o));
       if constexpr (MODE == GRAD_BEFORE) {
-        if (p.grad_other != nullptr) {
+        if (ALL || p.grad_other != nullptr) {
 #pragma unroll
           for (int c = 0; c < N; c++) o[c] *= p.scale;
-          store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
+          mine.store(p.grad_other + row, i, V::pack(o));
         }
       }
       if constexpr (kFull) {
-        if (p.grad_other != nullptr) {
+        if (ALL || p.grad_other != nullptr) {
 #pragma unroll
           for (int c = 0; c < N; c++) x[c] = 0.f;
           if (has_beta) V::unpack(beta[i], x);
 #pragma unroll
           for (int c = 0; c < N; c++) o[c] = p.scale * g[i][c] * fmaf(fmaf(v[i][c], r, minus), gamma[i][c], x[c]);
-          store_piece(p.grad_other + row, at[i], p.row_bytes, V::pack(o));
+          mine.store(p.grad_other + row, i, V::pack(o));
         }
       }
     }
@@ -348,8 +372,8 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
     if constexpr (W > 1) {
 #pragma unroll
       for (int i = 0; i < NV; i++) {
-        if (at[i] >= p.row_bytes) continue;
-        const size_t col = (size_t)blockIdx.x * p.H + piece_at(at[i], p.row_bytes) / V::kBytes;
+        if (mine.at[i] >= p.row_bytes) continue;
+        const size_t col = (size_t)blockIdx.x * p.H + piece_at(mine.at[i], p.row_bytes) / V::kBytes;
 #pragma unroll
         for (int c = 0; c < N; c++) part[col + c] = acc[i][c] * scale;
       }
@@ -444,7 +468,8 @@ uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
 
 template <int DT, bool AFTER, int W, int NV>
 hipError_t norm_as(const NormParams& p, hipStream_t st) {
-  hipLaunchKernelGGL((k_norm<DT, W, NV, AFTER>), dim3((unsigned)((p.T + rows_of<W>() - 1) / rows_of<W>())), dim3(threads_of<W>()), 0, st, p);
+  auto kernel = p.row_bytes == W * NV * 1024 ? k_norm<DT, W, NV, AFTER, true> : k_norm<DT, W, NV, AFTER, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + rows_of<W>() - 1) / rows_of<W>())), dim3(threads_of<W>()), 0, st, p);
   return hipGetLastError();
 }
 // Wavefronts a row and pieces a lane.  us for 1 / 512 / 16384 rows of 2048 columns, bf16: one wavefront 2.2 / 3.8 / 42.0, four 1.8 / 3.4 / 42.4; of 4096
@@ -473,8 +498,10 @@ hipError_t launch_norm(int dtype, const NormParams& p, hipStream_t st) {
 
 template <int DT, int MODE, bool WITH_B, int W, int NV>
 hipError_t norm_grad_as(const NormGradParams& p, hipStream_t st) {
-  hipLaunchKernelGGL((k_norm_grad<DT, W, NV, MODE, WITH_B, (W <= 8)>), dim3((unsigned)workgroups_of(p.T, pieces_of(p.row_bytes))),
-                     dim3(threads_of<W>()), 0, st, p);
+  constexpr bool PRE = W <= 8;
+  const bool given = MODE == GRAD_BEFORE ? p.more != nullptr && p.grad_other != nullptr : MODE != GRAD_AFTER_FULL || p.grad_other != nullptr;
+  auto kernel = given && p.row_bytes == W * NV * 1024 ? k_norm_grad<DT, W, NV, MODE, WITH_B, PRE, true> : k_norm_grad<DT, W, NV, MODE, WITH_B, PRE, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups_of(p.T, pieces_of(p.row_bytes))), dim3(threads_of<W>()), 0, st, p);
   return hipGetLastError();
 }
 // us for 16384 rows of 2048 columns, a full gate, with one wavefront a row 71, with four 64 (before the block 62 / 61); of 4096 columns, before
