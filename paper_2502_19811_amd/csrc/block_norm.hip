@@ -1,8 +1,8 @@
 // The norms on either side of the block, with the residual stream: sum and norm in front of it, norm, gate and residual sum
 // behind it, and their gradients.
 //
-// A row stays in registers between its loads and its stores: W wavefronts hold it, NV pieces of 16 bytes a lane, so that every
-// input is read once and every output written once.  Sums over a row are fp32, in a fixed order: lanes by DPP, wavefronts
+// A row stays in registers between its loads and its stores: one wavefront or a workgroup of up to MW hold it, NV pieces of 16 bytes a
+// lane, so that every input is read once and every output written once.  Sums over a row are fp32, in a fixed order: lanes by DPP, wavefronts
 // through LDS.  The mean of a "layer" norm is taken off before the squares are summed.
 #include "row_vector.h"
 
@@ -43,49 +43,60 @@ struct NormGradParams {
   float scale, eps, inv_h;
 };
 
-// Sums over the W wavefronts of a row, in every lane of them.  which (0, 1): one of two places in LDS; a wavefront may write the
-// sums of the next row while another still reads the last ones, so sums that follow each other take turns.
+// Workgroups: MW == 1 four wavefronts with a row each, otherwise a row for up to MW wavefronts, as many as the launch has.
+template <int MW> constexpr int threads_of() { return MW == 1 ? 256 : MW * 64; }
+template <int MW> __device__ __forceinline__ int row_waves() { return MW == 1 ? 1 : (int)(blockDim.x >> 6); }
+
+// What the wavefronts of a row tell each other: four places, each for up to 3 sums, which take turns -- a wavefront may write the next
+// sums while another still reads the last ones.  The places of wavefronts that the workgroup does not have hold zeros.
+template <int MW> struct RowSums { float part[4][3][MW]; };
+template <int MW>
+__device__ __forceinline__ void clear_absent(RowSums<MW>& sums) {
+  if constexpr (MW > 1) {
+    const int w = threadIdx.x % MW, at = threadIdx.x / MW;
+    if (w >= row_waves<MW>() && at < 12) (&sums.part[0][0][0])[at * MW + w] = 0.f;
+  }
+}
+// Sums over the wavefronts of a row, in every lane of them.
 // ragged: the last pieces of a row share bytes, perhaps across two wavefronts, and an output may lie in an input's place: what
 // was requested has to be there before any wavefront goes on to its stores.
-template <int W, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int which, bool ragged) {
+template <int MW, int N>
+__device__ __forceinline__ void row_sums(RowSums<MW>& sums, float (&v)[N], int place, bool ragged) {
   if (ragged) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
   for (int i = 0; i < N; i++) v[i] = wave_sum(v[i]);
-  if constexpr (W > 1) {
-    __shared__ float part[2][3][W];
+  if constexpr (MW > 1) {
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < N; i++) part[which][i][wave] = v[i];
+      for (int i = 0; i < N; i++) sums.part[place][i][wave] = v[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      float s = part[which][i][0];
+      float s = 0.f;
 #pragma unroll
-      for (int w = 1; w < W; w++) s += part[which][i][w];
+      for (int w = 0; w < MW; w += 4) s += (sums.part[place][i][w] + sums.part[place][i][w + 1]) + (sums.part[place][i][w + 2] + sums.part[place][i][w + 3]);
       v[i] = s;
     }
   }
 }
 
-template <int W> constexpr int threads_of() { return W > 4 ? W * 64 : 256; }
-template <int W> constexpr int rows_of() { return W > 4 ? 1 : 4 / W; }   // rows of a workgroup
-
-// A lane's pieces of a row.  EXACT: the row has W * NV * 64 of them, one for everybody.  Otherwise it has more than half as many (and with one
-// wavefront and at most two pieces a lane more than the last piece's beginning): the later pieces may lie behind its end, for some wavefronts.
-// Whether a wavefront has any of a piece, and all of it, is the same in its lanes: what is not there is neither loaded nor computed
-// (8192 rows of 4104 columns, eight wavefronts with two pieces a lane, behind the block: 49 us with all of them, 41 without).
-template <int DT, int W, int NV, bool EXACT>
+// A lane's pieces of a row.  EXACT: the row has as many as its wavefronts' lanes have places, one for everybody.  Otherwise the last
+// ones may lie behind its end, for some wavefronts: whether a wavefront has any of a piece, and all of it, is the same in its lanes, and
+// what is not there is neither loaded nor computed (8192 rows of 4104 columns, behind the block: 49 us with all of them, 41 without).
+// The launch takes no more wavefronts than it needs, so that all of them have any of their first pieces, and with NV > 1 all of the
+// first half of them.
+template <int DT, int MW, int NV, bool EXACT>
 struct Pieces {
   static constexpr int N = Row<DT>::kVec;
-  uint32_t at[NV], first, row_bytes;
-  __device__ __forceinline__ Pieces(int wave, int lane, uint32_t bytes) : first((uint32_t)(wave % W) * 1024), row_bytes(bytes) {
+  uint32_t at[NV], first, step, row_bytes;
+  __device__ __forceinline__ Pieces(int wave, int lane, uint32_t bytes)
+      : first(MW == 1 ? 0u : (uint32_t)wave * 1024), step((uint32_t)row_waves<MW>() * 1024), row_bytes(bytes) {
 #pragma unroll
-    for (int i = 0; i < NV; i++) at[i] = (uint32_t)(i * W * 1024) + first + lane * 16;
+    for (int i = 0; i < NV; i++) at[i] = i * step + first + lane * 16;
   }
-  __device__ __forceinline__ bool any(int i) const { return EXACT || i < NV / 2 || (W == 1 && NV <= 2) || (uint32_t)(i * W * 1024) + first < row_bytes; }
-  __device__ __forceinline__ bool all(int i) const { return EXACT || i < NV / 2 || (uint32_t)((i * W + 1) * 1024) + first <= row_bytes; }
+  __device__ __forceinline__ bool any(int i) const { return EXACT || NV == 1 || i < NV / 2 || (MW == 1 && NV <= 2) || i * step + first < row_bytes; }
+  __device__ __forceinline__ bool all(int i) const { return EXACT || i < NV / 2 || i * step + first + 1024 <= row_bytes; }
   __device__ __forceinline__ void store(char* row, int i, const u32x4& v) const {
     if constexpr (EXACT) *(u32x4*)(row + at[i]) = v;
     else store_piece(row, at[i], row_bytes, v);
@@ -120,16 +131,18 @@ struct Pieces {
 
 // n = v * r - mean * r, one fused operation an element whatever the norm: at 16 lanes a cycle and SIMD an operation on every element of
 // 16384 x 4096 takes 1.7 us, so the gradients, which read three rows, have room for about 30.
-template <int DT, int W, int NV, bool AFTER, bool EXACT>
-__global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
+template <int DT, int MW, int NV, bool AFTER, bool EXACT>
+__global__ __launch_bounds__(threads_of<MW>()) void k_norm(NormParams p) {
   using V = Row<DT>;
   constexpr int N = V::kVec;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int t = blockIdx.x * rows_of<W>() + wave / W;
-  if (t >= p.T) return;   // (W > 1: the whole workgroup or nobody)
+  const int t = MW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (t >= p.T) return;   // (MW > 1: the whole workgroup or nobody)
+  __shared__ RowSums<MW> sums;
+  clear_absent(sums);
   const size_t row = (size_t)t * p.row_bytes;
   const bool ragged = !EXACT && p.row_bytes % 16 != 0;
-  const Pieces<DT, W, NV, EXACT> mine(wave, lane, p.row_bytes);
+  const Pieces<DT, MW, NV, EXACT> mine(wave, lane, p.row_bytes);
   u32x4 rv[NV], bv[NV], gv[NV], hv[NV];
   if (!AFTER || p.residual != nullptr)
     mine.each([&](int i) { rv[i] = load_once(p.residual + row, mine.at[i], p.row_bytes); });
@@ -166,7 +179,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
   if (p.layer) {
     float s[1] = {0.f};
     mine.each_element([&](int i, int c, bool counts) { s[0] += counts ? v[i][c] : 0.f; });
-    row_sums<W>(s, 0, false);
+    row_sums<MW>(sums, s, 0, false);
     mean = s[0] * p.inv_h;
     mine.each_element([&](int i, int c, bool counts) {
       const float d = counts ? v[i][c] - mean : 0.f;
@@ -178,7 +191,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
       sq[0] = fmaf(d, d, sq[0]);
     });
   }
-  row_sums<W>(sq, 1, ragged);
+  row_sums<MW>(sums, sq, 1, ragged);
   const float r = 1.f / sqrtf(fmaf(sq[0], p.inv_h, p.eps)), minus = p.layer ? -mean * r : 0.f;
   if constexpr (!AFTER)
     if (p.sum != nullptr)
@@ -214,21 +227,23 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm(NormParams p) {
 // Gradients.  With n the normed row, e the gradient of n and r the reciprocal deviation, the gradient of the row is
 //   r * (e - mean(e) - n * mean(e * n))           (without the mean of e where no mean was taken off),
 // which is c1 * e + c2 * v + c0 with three numbers a row.  The scale and a token's gate are factors of these numbers.
-// A group of W wavefronts takes rows group, group + groups, ... and keeps, in registers, its columns' sums over them: A of
+// A group, the wavefronts that hold a row, takes rows group, group + groups, ... and keeps, in registers, its columns' sums over them: A of
 // f * n and B of f, f the gradient of gamma * n + beta but for the scale and a channel gate, which are factors of the sums; they go
 // to part_a and part_b, a row for each workgroup, which k_norm_columns adds up in a fixed order.  The next row is requested before the present one
 // is summed up (PRE), which the largest rows have no registers for.  Its loads are waited for by counting what was requested after them,
 // which takes that nothing is conditional: ALL says that the row is exact and that every optional row is given.
 enum { GRAD_BEFORE = 0, GRAD_AFTER = 1, GRAD_AFTER_TOKEN = 2, GRAD_AFTER_FULL = 3 };   // AFTER: no gate or a channel gate
-template <int DT, int W, int NV, int MODE, bool WITH_B, bool PRE, bool ALL>
-__global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p) {
+template <int DT, int MW, int NV, int MODE, bool WITH_B, bool PRE, bool ALL>
+__global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p) {
   using V = Row<DT>;
   constexpr int N = V::kVec;
   constexpr bool kToken = MODE == GRAD_AFTER_TOKEN, kFull = MODE == GRAD_AFTER_FULL;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int group = blockIdx.x * rows_of<W>() + wave / W;
+  const int group = MW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  __shared__ RowSums<MW> sums;
+  clear_absent(sums);
   const bool ragged = !ALL && p.row_bytes % 16 != 0;
-  const Pieces<DT, W, NV, ALL> mine(wave, lane, p.row_bytes);
+  const Pieces<DT, MW, NV, ALL> mine(wave, lane, p.row_bytes);
   float gamma[NV][N];   // with a channel gate multiplied in
   u32x4 beta[NV];
   const bool has_beta = (kToken || kFull) && p.beta != nullptr;
@@ -253,13 +268,19 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
       acc_a[i][c] = 0.f;
       if constexpr (WITH_B) acc_b[i][c] = 0.f;
     }
-  u32x4 vv[NV], gg[NV], hh[kFull ? NV : 1];
+  // A third row is read: the gate, or the stream's own gradient, which is needed last.  Requested with the others, a row ahead (LATE: when
+  // its turn begins), it takes registers and saves a wait where waits are for everything: 10000 rows of 4104 columns 109 us / 80 a row
+  // ahead, 16384 of 4096 121 / 126.
+  constexpr bool kThird = kFull || MODE == GRAD_BEFORE, kLate = MODE == GRAD_BEFORE && ALL;
+  const char* third = kFull ? p.gate : p.more;
+  const bool has_third = kThird && (ALL || third != nullptr);
+  u32x4 vv[NV], gg[NV], hh[kThird ? NV : 1];
   auto request = [&](int t) {
     const size_t row = (size_t)t * p.row_bytes;
     mine.each([&](int i) { vv[i] = load_once(p.v + row, mine.at[i], p.row_bytes); });
     mine.each([&](int i) { gg[i] = load_once(p.g + row, mine.at[i], p.row_bytes); });
-    if constexpr (kFull)
-      mine.each([&](int i) { hh[i] = load_once(p.gate + row, mine.at[i], p.row_bytes); });
+    if constexpr (kThird && !kLate)
+      if (has_third) mine.each([&](int i) { hh[i] = load_once(third + row, mine.at[i], p.row_bytes); });
   };
   int flip = 0;
   if constexpr (PRE)
@@ -267,16 +288,15 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
   for (int t = group; t < p.T; t += p.groups) {
     const size_t row = (size_t)t * p.row_bytes;
     if constexpr (!PRE) request(t);
-    u32x4 more[NV];   // what the stream's gradient is before
-    if constexpr (MODE == GRAD_BEFORE)
-      if (ALL || p.more != nullptr)
-        mine.each([&](int i) { more[i] = load_once(p.more + row, mine.at[i], p.row_bytes); });
+    u32x4 more[MODE == GRAD_BEFORE ? NV : 1];
+    if constexpr (kLate) mine.each([&](int i) { more[i] = load_once(third + row, mine.at[i], p.row_bytes); });
     float v[NV][N], f[NV][N], g[kFull ? NV : 1][N];   // f: gradient of gamma * n + beta, but for the factors said above
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       if (!mine.any(i)) continue;
       V::unpack(vv[i], v[i]);
       V::unpack(gg[i], f[i]);
+      if constexpr (MODE == GRAD_BEFORE && !kLate) more[i] = hh[i];
       if constexpr (kFull) {
         float h[N];
         V::unpack(hh[i], h);
@@ -298,7 +318,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
         m[0] += counts ? v[i][c] : 0.f;
         m[1] = fmaf(counts ? f[i][c] : 0.f, counts ? gamma[i][c] : 0.f, m[1]);
       });
-      row_sums<W>(m, flip, false);
+      row_sums<MW>(sums, m, 2 + flip, false);
       mean = m[0] * p.inv_h;
       sum_e = m[1];
       mine.each_element([&](int i, int c, bool counts) {
@@ -320,12 +340,12 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
         for (int i = 0; i < NV; i++) V::unpack(beta[i], b[i]);
         mine.each_element([&](int i, int c, bool counts) { s[2] = fmaf(counts ? f[i][c] : 0.f, counts ? b[i][c] : 0.f, s[2]); });
       }
-    row_sums<W>(s, flip, ragged);
+    row_sums<MW>(sums, s, flip, ragged);
     flip ^= 1;
     const float r = 1.f / sqrtf(fmaf(s[0], p.inv_h, p.eps)), minus = p.layer ? -mean * r : 0.f;
     const float en = s[1] * r;   // sum of e * n
     if constexpr (kToken)
-      if (p.grad_token_gate != nullptr && lane == 0 && wave % W == 0) p.grad_token_gate[t] = p.scale * (en + s[2]);
+      if (p.grad_token_gate != nullptr && lane == 0 && (MW == 1 || wave == 0)) p.grad_token_gate[t] = p.scale * (en + s[2]);
     const float c1 = MODE == GRAD_BEFORE ? r : r * p.scale * gate_t;
     const float c2 = -c1 * r * (en * p.inv_h);
     const float c0 = p.layer ? -c1 * (sum_e * p.inv_h) - c2 * mean : 0.f;
@@ -337,7 +357,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
       if constexpr (MODE == GRAD_BEFORE) {
 #pragma unroll
         for (int c = 0; c < N; c++) x[c] = 0.f;
-        if (ALL || p.more != nullptr) V::unpack(more[i], x);
+        if (has_third) V::unpack(more[i], x);
       }
 #pragma unroll
       for (int c = 0; c < N; c++) {
@@ -369,7 +389,7 @@ __global__ __launch_bounds__(threads_of<W>()) void k_norm_grad(NormGradParams p)
   if (p.part_a == nullptr) return;
   const float scale = MODE == GRAD_BEFORE ? 1.f : p.scale;
   auto leave = [&](float* part, float (&acc)[NV][N]) {
-    if constexpr (W > 1) {
+    if constexpr (MW > 1) {
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         if (mine.at[i] >= p.row_bytes) continue;
@@ -448,43 +468,50 @@ __global__ __launch_bounds__(1024) void k_norm_columns(NormColumnParams p) {
 
 namespace {
 
-// Groups of rows at most, with 1, 4, and 8 or 16 wavefronts a row.  More keep more rows on the way, but each workgroup's sums are written
-// and read: us for 16384 rows of 4096 columns, a full gate, with 512 / 768 / 1024 groups 130 + 4.9 / 146 + 6.1 / 138 + 7.2 (gradient + column
-// sums); for 30000 of 1024 with 4096 / 6144 59 + 6 / 59 + 8.
-constexpr int kGroups1 = 4096, kGroups4 = 512, kGroups8 = 256;
+uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
 
-// Wavefronts that hold a row, from its pieces of 16 bytes.
-int waves_of(uint32_t pieces) { return pieces <= 128 ? 1 : pieces <= 512 ? 4 : pieces <= 1024 ? 8 : 16; }
+// Pieces a lane and wavefronts of a row.  One wavefront up to 128 pieces; then one piece a lane, or two where that makes rows of up to 512
+// pieces come out even; two beyond, four beyond 2048.  us for 1 / 512 / 16384 rows: 2048 columns (256 pieces) one wavefront 2.2 / 3.8 / 42.0, four 1.8 /
+// 3.4 / 42.4; 4096 columns one 3.4 / 5.7 / 94.1, four 2.4 / 4.8 / 89.5, eight 2.1 / 4.7 / 86.7 (8192 rows with the update: 41.0 with four, 42.9 with
+// eight); gradient of 4096 rows of 3584 columns four of two pieces, some of them empty, 30.0, seven of one 26.8.
+struct RowShape { int nv, waves; };
+RowShape shape_of(uint32_t pieces) {
+  if (pieces <= 128) return {pieces <= 64 ? 1 : 2, 1};
+  const int nv = pieces > 2048 ? 4 : pieces > 512 || pieces % 128 == 0 ? 2 : 1;
+  return {nv, (int)((pieces + 64 * nv - 1) / (64 * nv))};
+}
+
+// Groups of rows of the gradients: per compute unit about 14 wavefronts with one piece a lane, 8 with two, which keeps enough rows on the
+// way and leaves few sums of columns to write and read; then as few as have as many rows each.  us for 10000 rows, before the block, sums of
+// columns included: 2049 columns (5 wavefronts of a piece) 1 / 2 / 4 groups a unit 82 / 58 / 53, behind it with a full gate 85 / 63 / 84; 4104
+// columns (5 of two) 1 / 2 85 / 90, 88 / 97; 3584 columns (7 of one) 4096 rows, 292 groups of 14 or 15 rows 36, 256 of 16 rows 31.
+constexpr int kGroups1 = 4096;   // one wavefront a row: us for 30000 rows of 1024 columns with 4096 / 6144 groups 65 / 67
 int groups_of(int T, uint32_t pieces) {
-  const int waves = waves_of(pieces), most = waves == 1 ? kGroups1 : waves == 4 ? kGroups4 : kGroups8;
-  return T < most ? T : most;
+  const RowShape s = shape_of(pieces);
+  const int a_unit = (s.nv == 1 ? 14 : 8) / s.waves, most = s.waves == 1 ? kGroups1 : kDefaultCus * (a_unit > 0 ? a_unit : 1);
+  if (T <= most) return T;
+  const int each = (T + most - 1) / most;
+  return (T + each - 1) / each;
 }
 // Workgroups of the gradients, each of which leaves a row of column sums.
 int workgroups_of(int T, uint32_t pieces) {
   const int groups = groups_of(T, pieces);
-  return waves_of(pieces) == 1 ? (groups + 3) / 4 : groups;
+  return shape_of(pieces).waves == 1 ? (groups + 3) / 4 : groups;
 }
-uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
 
-template <int DT, bool AFTER, int W, int NV>
-hipError_t norm_as(const NormParams& p, hipStream_t st) {
-  auto kernel = p.row_bytes == W * NV * 1024 ? k_norm<DT, W, NV, AFTER, true> : k_norm<DT, W, NV, AFTER, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + rows_of<W>() - 1) / rows_of<W>())), dim3(threads_of<W>()), 0, st, p);
+template <int DT, bool AFTER, int MW, int NV>
+hipError_t norm_as(const NormParams& p, int waves, hipStream_t st) {
+  auto kernel = p.row_bytes == (uint32_t)waves * NV * 1024 ? k_norm<DT, MW, NV, AFTER, true> : k_norm<DT, MW, NV, AFTER, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(MW == 1 ? (p.T + 3) / 4 : p.T)), dim3(MW == 1 ? 256 : waves * 64), 0, st, p);
   return hipGetLastError();
 }
-// Wavefronts a row and pieces a lane.  us for 1 / 512 / 16384 rows of 2048 columns, bf16: one wavefront 2.2 / 3.8 / 42.0, four 1.8 / 3.4 / 42.4; of 4096
-// columns: one wavefront 3.4 / 5.7 / 94.1, four 2.4 / 4.8 / 89.5, eight 2.1 / 4.7 / 86.7 (8192 rows, with the update: 41.0 with four, 42.9 with eight); of 8192 columns: four 2.8 / 7.4 / 176, eight 2.6 / 7.4 / 179,
-// sixteen 2.4 / 7.2 / 179.
 template <int DT, bool AFTER>
 hipError_t norm_type(const NormParams& p, hipStream_t st) {
-  const uint32_t n = pieces_of(p.row_bytes);
-  if (n <= 64) return norm_as<DT, AFTER, 1, 1>(p, st);
-  if (n <= 128) return norm_as<DT, AFTER, 1, 2>(p, st);
-  if (n <= 256) return norm_as<DT, AFTER, 1, 4>(p, st);
-  if (n <= 512) return norm_as<DT, AFTER, 4, 2>(p, st);
-  if (n <= 1024) return norm_as<DT, AFTER, 8, 2>(p, st);
-  if (n <= 2048) return norm_as<DT, AFTER, 16, 2>(p, st);
-  if constexpr (DT == MOE_FP32) return norm_as<DT, AFTER, 16, 4>(p, st);
+  const RowShape s = shape_of(pieces_of(p.row_bytes));
+  if (s.waves == 1) return s.nv == 1 ? norm_as<DT, AFTER, 1, 1>(p, 1, st) : norm_as<DT, AFTER, 1, 2>(p, 1, st);
+  if (s.waves <= 8 && s.nv <= 2) return s.nv == 1 ? norm_as<DT, AFTER, 8, 1>(p, s.waves, st) : norm_as<DT, AFTER, 8, 2>(p, s.waves, st);
+  if (s.nv == 2) return norm_as<DT, AFTER, 16, 2>(p, s.waves, st);
+  if constexpr (DT == MOE_FP32) return norm_as<DT, AFTER, 16, 4>(p, s.waves, st);
   return hipErrorInvalidValue;   // (no row of two-byte elements is that long)
 }
 template <bool AFTER>
@@ -496,26 +523,21 @@ hipError_t launch_norm(int dtype, const NormParams& p, hipStream_t st) {
   }
 }
 
-template <int DT, int MODE, bool WITH_B, int W, int NV>
-hipError_t norm_grad_as(const NormGradParams& p, hipStream_t st) {
-  constexpr bool PRE = W <= 8;
+template <int DT, int MODE, bool WITH_B, int MW, int NV>
+hipError_t norm_grad_as(const NormGradParams& p, int waves, hipStream_t st) {
+  constexpr bool PRE = MW <= 8;
   const bool given = MODE == GRAD_BEFORE ? p.more != nullptr && p.grad_other != nullptr : MODE != GRAD_AFTER_FULL || p.grad_other != nullptr;
-  auto kernel = given && p.row_bytes == W * NV * 1024 ? k_norm_grad<DT, W, NV, MODE, WITH_B, PRE, true> : k_norm_grad<DT, W, NV, MODE, WITH_B, PRE, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups_of(p.T, pieces_of(p.row_bytes))), dim3(threads_of<W>()), 0, st, p);
+  auto kernel = given && p.row_bytes == (uint32_t)waves * NV * 1024 ? k_norm_grad<DT, MW, NV, MODE, WITH_B, PRE, true> : k_norm_grad<DT, MW, NV, MODE, WITH_B, PRE, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups_of(p.T, pieces_of(p.row_bytes))), dim3(MW == 1 ? 256 : waves * 64), 0, st, p);
   return hipGetLastError();
 }
-// us for 16384 rows of 2048 columns, a full gate, with one wavefront a row 71, with four 64 (before the block 62 / 61); of 4096 columns, before
-// the block, with four 124, with eight and a piece a lane 127 (twice as many groups of eight: 129).
 template <int DT, int MODE, bool WITH_B>
 hipError_t norm_grad_b(const NormGradParams& p, hipStream_t st) {
-  const uint32_t n = pieces_of(p.row_bytes);
-  if (n <= 64) return norm_grad_as<DT, MODE, WITH_B, 1, 1>(p, st);
-  if (n <= 128) return norm_grad_as<DT, MODE, WITH_B, 1, 2>(p, st);
-  if (n <= 256) return norm_grad_as<DT, MODE, WITH_B, 4, 1>(p, st);
-  if (n <= 512) return norm_grad_as<DT, MODE, WITH_B, 4, 2>(p, st);
-  if (n <= 1024) return norm_grad_as<DT, MODE, WITH_B, 8, 2>(p, st);
-  if (n <= 2048) return norm_grad_as<DT, MODE, WITH_B, 16, 2>(p, st);
-  if constexpr (DT == MOE_FP32) return norm_grad_as<DT, MODE, WITH_B, 16, 4>(p, st);
+  const RowShape s = shape_of(pieces_of(p.row_bytes));
+  if (s.waves == 1) return s.nv == 1 ? norm_grad_as<DT, MODE, WITH_B, 1, 1>(p, 1, st) : norm_grad_as<DT, MODE, WITH_B, 1, 2>(p, 1, st);
+  if (s.waves <= 8 && s.nv <= 2) return s.nv == 1 ? norm_grad_as<DT, MODE, WITH_B, 8, 1>(p, s.waves, st) : norm_grad_as<DT, MODE, WITH_B, 8, 2>(p, s.waves, st);
+  if (s.nv == 2) return norm_grad_as<DT, MODE, WITH_B, 16, 2>(p, s.waves, st);
+  if constexpr (DT == MOE_FP32) return norm_grad_as<DT, MODE, WITH_B, 16, 4>(p, s.waves, st);
   return hipErrorInvalidValue;   // (no row of two-byte elements is that long)
 }
 template <int DT>
