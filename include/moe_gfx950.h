@@ -299,7 +299,7 @@ int moe_last_device_status(const moe_plan_t *plan, const void *workspace, void *
  * result is rounded once.  The same call gives the same bits every time.  No plan, and no state between calls: workspaces are
  * scratch, and calls that may overlap in time need one each.
  * Supported: T >= 0; 8 <= H <= 65536 (norms: 16384), odd H included; 1 <= k <= 64, E <= 256, T*k < 2^24 (norms: T < 2^24),
- * T*H*(bytes of an element) < 2^36; anything else is MOE_ERR_UNSUPPORTED.  Row offsets are 64-bit.  With T = 0 the row pointers may be
+ * T*H*(bytes of an element) < 2^35; anything else is MOE_ERR_UNSUPPORTED.  Row offsets are 64-bit.  With T = 0 the row pointers may be
  * NULL, and what sums over tokens is written as zeros.  Outputs must not overlap inputs or each other except where said.
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef enum { MOE_BF16 = 0, MOE_FP16 = 1, MOE_FP32 = 2 } moe_dtype_t;

@@ -575,7 +575,7 @@ int norm_call(int32_t T, int32_t H, int32_t dtype, int32_t norm, float eps, floa
   if (!(eps >= 0.f) || !(eps < 1e30f) || !(scale > -1e30f && scale < 1e30f)) return MOE_ERR_INVALID_ARG;
   const int rc = norm_shape(T, H);
   if (rc != MOE_OK) return rc;
-  return (int64_t)T * H * element_bytes(dtype) < (1ll << 36) ? MOE_OK : MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
+  return (int64_t)T * H * element_bytes(dtype) < (1ll << 35) ? MOE_OK : MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
 }
 bool gate_ok(const void* gate, int32_t gate_kind, bool rows) {
   if (gate_kind < MOE_GATE_NONE || gate_kind > MOE_GATE_FULL) return false;

@@ -538,7 +538,7 @@ constexpr int kSortOwnSums = 32768;   // chunks x buckets
 int row_call(int32_t T, int32_t H, int32_t k, int32_t dtype, void* hip_stream, RowCall* c) {
   if (T < 0 || H <= 0 || k <= 0 || element_bytes(dtype) == 0) return MOE_ERR_INVALID_ARG;
   if (k > kMaxGateTopK || H < kMinRowColumns || H > kMaxRowColumns || (int64_t)T * k >= (1 << 24)) return MOE_ERR_UNSUPPORTED;
-  if ((int64_t)T * H * element_bytes(dtype) >= (1ll << 36)) return MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
+  if ((int64_t)T * H * element_bytes(dtype) >= (1ll << 35)) return MOE_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
   c->T = T;
   c->k = k;
   c->R = T * k;

@@ -1,5 +1,5 @@
 """The norms on either side of the block and their gradients against definitions in 64 bits: every number of wavefronts a row may
-have, rows of odd lengths and rows that do not fill their lanes, more rows than groups, every gate, outputs in the place of inputs."""
+have, rows of odd lengths and rows that do not fill their lanes, more rows than groups of rows, every gate, outputs in the place of inputs."""
 import itertools
 
 import pytest
@@ -10,8 +10,8 @@ import row_ops as ro
 pytestmark = pytest.mark.gpu
 
 EPS = 1e-5
-# bf16 pieces of 16 bytes: 1, 2, 64, 65, 126, 250, 251, 448, 512, 513, 577 (the last piece alone in its wavefront), 1025, 2048
-WIDTHS = [8, 9, 33, 512, 513, 1003, 2000, 2561, 3584, 4096, 4097, 4609, 8200, 16384]
+# bf16 pieces of 16 bytes: 1, 2, 5, 64, 65, 126, 138, 250, 256, 321 (the last piece alone in its wavefront), 448, 512, 513, 577, 1025, 2048
+WIDTHS = [8, 9, 33, 512, 513, 1003, 1100, 2000, 2048, 2561, 3584, 4096, 4097, 4609, 8200, 16384]
 CASES = [(1, False), (5, True), (300, False), (301, True)]
 GATES = ["none", "channel", "token", "full"]
 

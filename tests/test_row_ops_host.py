@@ -47,13 +47,13 @@ for name, base in CALLS.items():
 for name in ROWS:
     REFUSED += [(name, dict(H=0), INVALID), (name, dict(k=0), INVALID), (name, dict(dtype=3), INVALID), (name, dict(dtype=-1), INVALID),
                 (name, dict(H=7), UNSUPPORTED), (name, dict(H=65537), UNSUPPORTED), (name, dict(k=65), UNSUPPORTED),
-                (name, dict(T=1 << 23, k=2), UNSUPPORTED), (name, dict(T=1 << 20, k=1, H=32768, dtype=0), UNSUPPORTED)]
+                (name, dict(T=1 << 23, k=2), UNSUPPORTED), (name, dict(T=1 << 20, k=1, H=16384, dtype=0), UNSUPPORTED)]
 for name in NORMS:
     REFUSED += [(name, dict(H=0), INVALID), (name, dict(dtype=3), INVALID), (name, dict(norm=2), INVALID), (name, dict(norm=-1), INVALID),
                 (name, dict(eps=-1e-9), INVALID), (name, dict(eps=float("nan")), INVALID), (name, dict(eps=float("inf")), INVALID),
                 (name, dict(scale=float("nan")), INVALID), (name, dict(scale=float("inf")), INVALID),
                 (name, dict(H=7), UNSUPPORTED), (name, dict(H=16385), UNSUPPORTED), (name, dict(T=1 << 24), UNSUPPORTED),
-                (name, dict(T=1 << 21, H=16384, dtype=0), UNSUPPORTED)]
+                (name, dict(T=1 << 20, H=16384, dtype=0), UNSUPPORTED), (name, dict(T=1 << 20, H=8192, dtype=2), UNSUPPORTED)]
 for name in ("moe_sort_tokens", "moe_route_topk_backward"):
     REFUSED += [(name, dict(E=0), INVALID), (name, dict(k=0), INVALID), (name, dict(E=257), UNSUPPORTED),
                 (name, dict(T=1 << 23), UNSUPPORTED)]
