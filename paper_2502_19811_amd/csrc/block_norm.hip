@@ -283,9 +283,10 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p
       if (has_third) mine.each([&](int i) { hh[i] = load_once(third + row, mine.at[i], p.row_bytes); });
   };
   int flip = 0;
+  const int begin = group < p.groups ? group : p.T;   // (a wavefront beyond the groups has no rows)
   if constexpr (PRE)
-    if (group < p.T) request(group);
-  for (int t = group; t < p.T; t += p.groups) {
+    if (begin < p.T) request(begin);
+  for (int t = begin; t < p.T; t += p.groups) {
     const size_t row = (size_t)t * p.row_bytes;
     if constexpr (!PRE) request(t);
     u32x4 more[MODE == GRAD_BEFORE ? NV : 1];
