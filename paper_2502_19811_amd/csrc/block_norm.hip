@@ -584,7 +584,11 @@ bool gate_ok(const void* gate, int32_t gate_kind, bool rows) {
   return (gate != nullptr || (!rows && gate_kind != MOE_GATE_CHANNEL)) && aligned16(gate);
 }
 // An output may lie in the place of an input of the same rows, not across it.
-bool apart(const void* out, const void* in, size_t bytes) { return !out || !in || out == in || !overlap(out, bytes, in, bytes); }
+bool in_place_or_apart(const void* out, std::initializer_list<const void*> ins, size_t bytes) {
+  for (const void* in : ins)
+    if (out != in && overlap({out, bytes}, {in, bytes})) return false;
+  return true;
+}
 
 int status_of(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
@@ -605,9 +609,9 @@ int moe_norm_before(const void* residual, const void* update, float residual_sca
   if (!aligned16(residual) || !aligned16(update) || !aligned16(gamma) || !aligned16(beta) || !aligned16(sum) || !aligned16(x))
     return MOE_ERR_INVALID_ARG;
   const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
-  if (!apart(sum, residual, bytes) || !apart(sum, update, bytes) || !apart(x, residual, bytes) || !apart(x, update, bytes))
+  if (!in_place_or_apart(sum, {residual, update}, bytes) || !in_place_or_apart(x, {residual, update}, bytes) ||
+      !apart({{sum, bytes}, {x, bytes}}, {{gamma, row_bytes}, {beta, row_bytes}}))
     return MOE_ERR_INVALID_ARG;
-  if (sum && overlap(sum, bytes, x, bytes)) return MOE_ERR_INVALID_ARG;
   NormParams p = {};
   p.residual = (const char*)residual;
   p.branch = (const char*)update;
@@ -633,7 +637,10 @@ int moe_norm_after(const void* residual, const void* y, const void* gamma, const
   if (!y || !gamma || !out) return MOE_ERR_INVALID_ARG;
   if (!aligned16(residual) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
   const size_t row_bytes = (size_t)H * element_bytes(dtype), bytes = T * row_bytes;
-  if (!apart(out, residual, bytes) || !apart(out, y, bytes) || (gate_kind == MOE_GATE_FULL && !apart(out, gate, bytes))) return MOE_ERR_INVALID_ARG;
+  const bool full = gate_kind == MOE_GATE_FULL;
+  const Span small_gate = {full ? nullptr : gate, gate_kind == MOE_GATE_TOKEN ? (size_t)T * 4 : row_bytes};
+  if (!in_place_or_apart(out, {residual, y, full ? gate : nullptr}, bytes) || !apart({{out, bytes}}, {{gamma, row_bytes}, {beta, row_bytes}, small_gate}))
+    return MOE_ERR_INVALID_ARG;
   NormParams p = {};
   p.residual = (const char*)residual;
   p.branch = (const char*)y;
@@ -669,10 +676,13 @@ int moe_norm_before_backward(const void* sum, const void* gamma, const void* gra
   if (!aligned16(sum) || !aligned16(gamma) || !aligned16(grad_x) || !aligned16(grad_sum) || !aligned16(grad_residual) ||
       !aligned16(grad_update) || !aligned16(grad_gamma) || !aligned16(grad_beta) || !aligned16(workspace))
     return MOE_ERR_INVALID_ARG;
-  if (columns && workspace_bytes < moe_norm_workspace_bytes(T, H)) return MOE_ERR_WORKSPACE_TOO_SMALL;
-  for (void* out : {grad_residual, grad_update})
-    if (!apart(out, sum, bytes) || !apart(out, grad_x, bytes) || !apart(out, grad_sum, bytes)) return MOE_ERR_INVALID_ARG;
-  if (grad_update && T > 0 && overlap(grad_update, bytes, grad_residual, bytes)) return MOE_ERR_INVALID_ARG;
+  const size_t scratch = columns ? moe_norm_workspace_bytes(T, H) : 0, sums = (size_t)H * 4;
+  if (workspace_bytes < scratch) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  const Span small[3] = {{grad_gamma, sums}, {grad_beta, sums}, {columns ? workspace : nullptr, scratch}};
+  if (!in_place_or_apart(grad_residual, {sum, grad_x, grad_sum}, bytes) || !in_place_or_apart(grad_update, {sum, grad_x, grad_sum}, bytes) ||
+      !apart({{grad_residual, bytes}, {grad_update, bytes}, small[0], small[1], small[2]}, {{gamma, row_bytes}}) ||
+      !apart({small[0], small[1], small[2]}, {{sum, bytes}, {grad_x, bytes}, {grad_sum, bytes}}))
+    return MOE_ERR_INVALID_ARG;
   NormGradParams p = {};
   p.v = (const char*)sum;
   p.g = (const char*)grad_x;
@@ -714,11 +724,16 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   if (!aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(grad_out) || !aligned16(grad_y) || !aligned16(grad_gamma) ||
       !aligned16(grad_beta) || !aligned16(grad_gate) || !aligned16(workspace))
     return MOE_ERR_INVALID_ARG;
-  if (columns && workspace_bytes < moe_norm_workspace_bytes(T, H)) return MOE_ERR_WORKSPACE_TOO_SMALL;
-  const bool full = gate_kind == MOE_GATE_FULL;
-  for (void* out : {grad_y, full ? grad_gate : nullptr})
-    if (!apart(out, y, bytes) || !apart(out, grad_out, bytes) || (full && !apart(out, gate, bytes))) return MOE_ERR_INVALID_ARG;
-  if (full && grad_gate && T > 0 && overlap(grad_gate, bytes, grad_y, bytes)) return MOE_ERR_INVALID_ARG;
+  const size_t scratch = columns ? moe_norm_workspace_bytes(T, H) : 0, sums = (size_t)H * 4;
+  if (workspace_bytes < scratch) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  const bool full = gate_kind == MOE_GATE_FULL, token = gate_kind == MOE_GATE_TOKEN;
+  const Span small[4] = {{grad_gamma, sums}, {grad_beta, sums}, {columns ? workspace : nullptr, scratch}, {full ? nullptr : grad_gate, token ? (size_t)T * 4 : sums}};
+  const void *full_gate = full ? gate : nullptr, *grad_full = full ? grad_gate : nullptr;
+  if (!in_place_or_apart(grad_y, {y, grad_out, full_gate}, bytes) || !in_place_or_apart(grad_full, {y, grad_out, full_gate}, bytes) ||
+      !apart({{grad_y, bytes}, {grad_full, bytes}, small[0], small[1], small[2], small[3]},
+             {{gamma, row_bytes}, {beta, row_bytes}, {full ? nullptr : gate, token ? (size_t)T * 4 : row_bytes}}) ||
+      !apart({small[0], small[1], small[2], small[3]}, {{y, bytes}, {grad_out, bytes}, {full_gate, bytes}}))
+    return MOE_ERR_INVALID_ARG;
   NormGradParams p = {};
   p.v = (const char*)y;
   p.g = (const char*)grad_out;
@@ -728,7 +743,7 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   p.gate_kind = gate_kind;
   p.grad_v = (char*)grad_y;
   p.grad_other = full ? (char*)grad_gate : nullptr;
-  p.grad_token_gate = gate_kind == MOE_GATE_TOKEN ? (float*)grad_gate : nullptr;
+  p.grad_token_gate = token ? (float*)grad_gate : nullptr;
   p.layer = norm == MOE_NORM_LAYER;
   p.T = T;
   p.H = H;
@@ -750,7 +765,7 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   cp.grad_gate = channel ? (float*)grad_gate : nullptr;
   cp.groups = workgroups_of(T, pieces_of(p.row_bytes));
   cp.H = H;
-  const int mode = full ? GRAD_AFTER_FULL : gate_kind == MOE_GATE_TOKEN ? GRAD_AFTER_TOKEN : GRAD_AFTER;
+  const int mode = full ? GRAD_AFTER_FULL : token ? GRAD_AFTER_TOKEN : GRAD_AFTER;
   return status_of(launch_norm_grad(dtype, mode, p, cp, (hipStream_t)hip_stream));
 }
 

@@ -4,6 +4,8 @@
 // the alignment of its element: global memory instructions of gfx950 take any.  The last piece of a row that is not a multiple
 // of 16 bytes lies over the one before it, which needs no code of its own for what is left.
 #pragma once
+#include <initializer_list>
+
 #include "moe_device.h"
 
 namespace moe {
@@ -109,9 +111,20 @@ inline int element_bytes(int dtype) { return dtype == MOE_BF16 || dtype == MOE_F
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Whether two buffers share bytes.
-inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
-  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+// Whether two buffers share bytes; a buffer that is not given shares none.
+struct Span { const void* at; size_t bytes; };
+inline bool overlap(const Span& a, const Span& b) {
+  return a.at && b.at && (uintptr_t)a.at < (uintptr_t)b.at + b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + a.bytes;
+}
+// Whether no output shares bytes with another output or with an input.
+inline bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* a = outs.begin(); a != outs.end(); a++) {
+    for (const Span* b = outs.begin(); b != a; b++)
+      if (overlap(*a, *b)) return false;
+    for (const Span& b : ins)
+      if (overlap(*a, b)) return false;
+  }
+  return true;
 }
 
 }  // namespace moe

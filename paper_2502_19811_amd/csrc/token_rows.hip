@@ -438,6 +438,7 @@ struct RowCall {
   hipStream_t st;
   size_t token_bytes() const { return (size_t)T * row_bytes; }
   size_t rows_bytes() const { return (size_t)R * row_bytes; }
+  size_t pair_bytes() const { return (size_t)R * 4; }
 };
 
 // Lanes of a token, as many as a row has pieces.  us for 32768 tokens of 64 columns, k = 2, with 8 lanes / 64: combine 3.9 / 8.6, its gradient
@@ -581,7 +582,9 @@ int moe_sort_tokens(const int32_t* topk_ids, int32_t T, int32_t E, int32_t k, in
   }
   if (!topk_ids || !perm || !inv_perm || !workspace) return MOE_ERR_INVALID_ARG;
   if (!aligned16(topk_ids) || !aligned16(perm) || !aligned16(inv_perm) || !aligned16(workspace)) return MOE_ERR_INVALID_ARG;
-  if (workspace_bytes < moe_sort_workspace_bytes(T, E, k)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  const size_t need = moe_sort_workspace_bytes(T, E, k), pairs = (size_t)R * 4;
+  if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  if (!apart({{expert_offsets, (size_t)(E + 1) * 4}, {perm, pairs}, {inv_perm, pairs}, {workspace, need}}, {{topk_ids, pairs}})) return MOE_ERR_INVALID_ARG;
   int32_t* hist = (int32_t*)workspace;
   const int n_chunks = n_chunks_of(R);
   if (n_chunks <= kSortOwnCounts) {
@@ -602,7 +605,7 @@ int moe_dispatch(const void* x, const int32_t* inv_perm, int32_t T, int32_t H, i
   if (rc != MOE_OK) return rc;
   if (T == 0) return MOE_OK;
   if (!x || !inv_perm || !rows || !aligned16(x) || !aligned16(inv_perm) || !aligned16(rows)) return MOE_ERR_INVALID_ARG;
-  if (overlap(x, c.token_bytes(), rows, c.rows_bytes())) return MOE_ERR_INVALID_ARG;
+  if (!apart({{rows, c.rows_bytes()}}, {{x, c.token_bytes()}, {inv_perm, c.pair_bytes()}})) return MOE_ERR_INVALID_ARG;
   return status_of(launch_dispatch(c, x, inv_perm, rows));
 }
 
@@ -614,7 +617,7 @@ int moe_combine(const void* rows, const int32_t* inv_perm, const float* topk_wei
   if (T == 0) return MOE_OK;
   if (!rows || !inv_perm || !out || !aligned16(rows) || !aligned16(inv_perm) || !aligned16(out) || !aligned16(topk_weights))
     return MOE_ERR_INVALID_ARG;
-  if (overlap(rows, c.rows_bytes(), out, c.token_bytes())) return MOE_ERR_INVALID_ARG;
+  if (!apart({{out, c.token_bytes()}}, {{rows, c.rows_bytes()}, {inv_perm, c.pair_bytes()}, {topk_weights, c.pair_bytes()}})) return MOE_ERR_INVALID_ARG;
   return status_of(launch_combine_rows(dtype, c, rows, inv_perm, topk_weights, out));
 }
 
@@ -633,7 +636,8 @@ int moe_combine_backward(const void* grad_out, const void* rows, const int32_t* 
   if (!aligned16(grad_out) || !aligned16(rows) || !aligned16(inv_perm) || !aligned16(topk_weights) || !aligned16(grad_rows) ||
       !aligned16(grad_weights))
     return MOE_ERR_INVALID_ARG;
-  if (overlap(grad_out, c.token_bytes(), grad_rows, c.rows_bytes()) || (rows && overlap(rows, c.rows_bytes(), grad_rows, c.rows_bytes())))
+  if (!apart({{grad_rows, c.rows_bytes()}, {grad_weights, c.pair_bytes()}},
+             {{grad_out, c.token_bytes()}, {rows, c.rows_bytes()}, {inv_perm, c.pair_bytes()}, {topk_weights, c.pair_bytes()}}))
     return MOE_ERR_INVALID_ARG;
   if (!grad_weights) rows = nullptr;
   switch (dtype) {
@@ -650,6 +654,8 @@ int moe_route_topk_backward(const int32_t* topk_ids, const float* topk_weights, 
   if (T == 0) return MOE_OK;
   if (!topk_ids || !topk_weights || !grad_weights || !grad_logits) return MOE_ERR_INVALID_ARG;
   if (!aligned16(topk_ids) || !aligned16(topk_weights) || !aligned16(grad_weights) || !aligned16(grad_logits)) return MOE_ERR_INVALID_ARG;
+  const size_t pairs = (size_t)T * k * 4;
+  if (!apart({{grad_logits, (size_t)T * E * 4}}, {{topk_ids, pairs}, {topk_weights, pairs}, {grad_weights, pairs}})) return MOE_ERR_INVALID_ARG;
   const int quads = (E + 3) / 4;
   const int64_t n_units = (int64_t)T * quads;
   auto kernel = k <= 2 ? k_route_topk_grad<2> : k <= 4 ? k_route_topk_grad<4> : k_route_topk_grad<8>;

@@ -80,6 +80,25 @@ REFUSED += [
     ("moe_norm_after_backward", dict(grad_y=D + 512), INVALID),
     ("moe_norm_after_backward", dict(gate=F + (1 << 37), gate_kind=3, grad_gate=E_), INVALID),
     ("moe_norm_after_backward", dict(ws_bytes=moe.moe_norm_workspace_bytes(100, 256) - 1), TOO_SMALL),
+    ("moe_sort_tokens", dict(inv=A), INVALID),
+    ("moe_sort_tokens", dict(perm=E_ + 400), INVALID),
+    ("moe_sort_tokens", dict(ws=B), INVALID),
+    ("moe_dispatch", dict(rows=B), INVALID),
+    ("moe_combine", dict(out=D), INVALID),
+    ("moe_combine_backward", dict(grad_weights=E_), INVALID),
+    ("moe_combine_backward", dict(grad_weights=F + 512), INVALID),
+    ("moe_route_topk_backward", dict(grad_logits=B), INVALID),
+    ("moe_norm_before", dict(x=D), INVALID),
+    ("moe_norm_before", dict(sum=D), INVALID),
+    ("moe_norm_before_backward", dict(grad_gamma=B), INVALID),
+    ("moe_norm_before_backward", dict(grad_gamma=D), INVALID),
+    ("moe_norm_before_backward", dict(grad_beta=F), INVALID),
+    ("moe_norm_before_backward", dict(ws=A), INVALID),
+    ("moe_norm_after", dict(gate=F, gate_kind=1, out=F), INVALID),
+    ("moe_norm_after", dict(out=D), INVALID),
+    ("moe_norm_after_backward", dict(grad_gamma=E_ + 512), INVALID),
+    ("moe_norm_after_backward", dict(gate=A + (1 << 37), gate_kind=2, grad_gate=A + (1 << 37)), INVALID),
+    ("moe_norm_after_backward", dict(gate=A + (1 << 37), gate_kind=1, grad_gate=F), INVALID),
     # gates that do not fit their kind
     ("moe_norm_after", dict(gate_kind=4), INVALID),
     ("moe_norm_after", dict(gate_kind=-1), INVALID),
