@@ -531,9 +531,9 @@ int n_chunks_of(int64_t R) { return (int)((R + kSortChunk - 1) / kSortChunk); }
 // Where a chunk's workgroup has the counts of the others from.  us, it counts all pairs itself / counts by a launch of their own:
 // 16384 pairs of 64 experts 5.4 / 6.8, 32768 6.5 / 7.2, 65536 8.7 / 7.1, of 8 experts 12.4 / 6.7; a launch also takes 2.6 us of the host.
 constexpr int kSortOwnCounts = 32;
-// It sums the counts of the chunks itself while they are few: 256 chunks of 65 buckets 6.9, 512 of 257 28, against 3.4 and 9 for 1024 chunks
-// of 9 buckets with their prefix sums by a launch of their own.
-constexpr int kSortOwnSums = 32768;   // chunks x buckets
+// It sums the counts of the chunks itself while they are few.  us of the scatter, itself / prefix sums by a launch of their own and the
+// scatter: 256 chunks of 65 buckets 6.9 / -, 512 of 257 28 / 5 + 7, 1024 of 9 14.4 / 3.4 + 8.8.
+constexpr int kSortOwnSums = 32768, kSortOwnSumChunks = 512;   // chunks x buckets, chunks
 
 // Checks that the row operators share; *c is set where there is something to do.
 int row_call(int32_t T, int32_t H, int32_t k, int32_t dtype, void* hip_stream, RowCall* c) {
@@ -591,7 +591,7 @@ int moe_sort_tokens(const int32_t* topk_ids, int32_t T, int32_t E, int32_t k, in
     hipLaunchKernelGGL(k_sort_scatter<true>, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, nullptr, n_chunks, nullptr, expert_offsets, perm, inv_perm);
     return status_of(hipGetLastError());
   }
-  int32_t* total = (int64_t)n_chunks * (E + 1) > kSortOwnSums ? hist + (size_t)n_chunks * (E + 1) : nullptr;
+  int32_t* total = n_chunks > kSortOwnSumChunks || n_chunks * (E + 1) > kSortOwnSums ? hist + (size_t)n_chunks * (E + 1) : nullptr;
   hipLaunchKernelGGL(k_sort_hist, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist);
   if (total) hipLaunchKernelGGL(k_sort_scan, dim3(E + 1), dim3(1024), 0, st, hist, n_chunks, E, total);
   hipLaunchKernelGGL(k_sort_scatter<false>, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, hist, n_chunks, total, expert_offsets, perm, inv_perm);
