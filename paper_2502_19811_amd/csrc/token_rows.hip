@@ -288,21 +288,23 @@ __global__ __launch_bounds__(256) void k_combine_rows(const char* rows, const in
 }
 
 // grad_rows[inv[t][j]] = w[t][j] * g[t], grad_w[t][j] = <g[t], rows[inv[t][j]]>, 0 for a slot without a row.  A token belongs to
-// WAVES wavefronts of one workgroup (LP == 64), which take its pieces in turn and add their sums up in LDS, or to LP lanes.
+// the wavefronts of a workgroup (LP == 64), which take its pieces in turn and add their sums up in LDS, or to LP lanes.
 // rows == nullptr: no grad_w.
-template <int DT, int K, int LP, int NV, int WAVES>
-__global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char* rows, const int32_t* __restrict__ inv,
+constexpr int kGradWaves = 8;
+template <int DT, int K, int LP, int NV>
+__global__ __launch_bounds__(LP == 64 ? kGradWaves * 64 : 256) void k_combine_grad(const char* g, const char* rows, const int32_t* __restrict__ inv,
                                                       const float* __restrict__ w, char* grad_rows, float* __restrict__ grad_w, int T,
                                                       int k, int R, uint32_t row_bytes) {
   using V = Row<DT>;
   constexpr int N = V::kVec, KK = K > 0 ? K : 1;
-  constexpr uint32_t kStep = WAVES * LP * 16 * NV;
-  __shared__ float part[WAVES > 1 ? KK : 1][4];
+  constexpr bool kWhole = LP == 64;   // a workgroup has one token
+  __shared__ float part[kWhole ? KK : 1][kGradWaves];
   Unit<LP> at(1);
-  if constexpr (WAVES > 1) at.t = blockIdx.x;
-  if (at.t >= T) return;   // (WAVES > 1: the whole workgroup or nobody)
+  if constexpr (kWhole) at.t = blockIdx.x;
+  if (at.t >= T) return;   // (kWhole: nobody)
+  const uint32_t step = kWhole ? blockDim.x * (16 * NV) : LP * 16 * NV;
   const char* src = g + (size_t)at.t * row_bytes;
-  const bool exact = row_bytes % kStep == 0;
+  const bool exact = row_bytes % step == 0;
   for (int j0 = 0; j0 < k; j0 += K > 0 ? k : 1) {
     int pos[KK];
     float wj[KK], dot[KK];
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char*
       wj[j] = there && w != nullptr ? w[(size_t)at.t * k + j0 + j] : 1.f;
       dot[j] = 0.f;
     }
-    for (uint32_t base = WAVES > 1 ? at.wave * (64 * 16 * NV) : 0; base < row_bytes; base += kStep) {
+    for (uint32_t base = kWhole ? at.wave * (64 * 16 * NV) : 0; base < row_bytes; base += step) {
       const uint32_t start = base + at.lane * 16;
       u32x4 gv[NV], rv[KK][NV];
 #pragma unroll
@@ -360,16 +362,20 @@ __global__ __launch_bounds__(256) void k_combine_grad(const char* g, const char*
 #pragma unroll
         for (int off = LP / 2; off >= 1; off >>= 1) dot[j] += __shfl_xor(dot[j], off);
       }
-      if constexpr (WAVES == 1) {
+      if constexpr (!kWhole) {
         if (at.lane == 0 && (K == 0 || j < k)) grad_w[(size_t)at.t * k + j0 + j] = dot[j];
       } else {
         if (at.lane == 0) part[j][at.wave] = dot[j];
       }
     }
-    if constexpr (WAVES > 1) {
+    if constexpr (kWhole) {
       __syncthreads();
       const int j = threadIdx.x;
-      if (j < KK && j0 + j < k) grad_w[(size_t)at.t * k + j0 + j] = (part[j][0] + part[j][1]) + (part[j][2] + part[j][3]);
+      if (j < KK && j0 + j < k) {
+        float sum = part[j][0];
+        for (int w = 1; w < (int)(blockDim.x >> 6); w++) sum += part[j][w];
+        grad_w[(size_t)at.t * k + j0 + j] = sum;
+      }
       if constexpr (K == 0) __syncthreads();   // part is written again
     }
   }
@@ -498,24 +504,27 @@ hipError_t launch_combine_rows(int dtype, const RowCall& c, const void* rows, co
   }
 }
 
-template <int DT, int K, int LP, int NV, int WAVES>
+// A token has up to 8 wavefronts with a piece a lane each, two where that is too few, so that its pieces are requested together.  us with one
+// wavefront a token and 1 / 2 / 4 pieces a lane, which takes longer rows in turns: 32768 tokens of 4096 columns, k = 2 284 / 287 / 268; so: 232.  With
+// always four: 12000 of 300 15.2, so 10.7, of 1500, k = 1 20.8 / 22.1, of 2600, k = 3 90.9 / 82.3, of 2339 in fp32, k = 5 280 / 256; 2048 of 3584, k = 8
+// 47.9 / 46.5.  Two pieces a lane from 2048 / 4096 / 8192 bytes a row: 12000 of 2600 91.5 / 92.3 / 82.3, 12000 of 2048, k = 4 80.9 / 76.8 / 76.2.
+template <int DT, int K, int LP, int NV>
 hipError_t combine_grad_as(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
-  const int64_t blocks = WAVES > 1 ? c.T : (((int64_t)c.T * LP + 63) / 64 + 3) / 4;
-  hipLaunchKernelGGL((k_combine_grad<DT, K, LP, NV, WAVES>), dim3((unsigned)blocks), dim3(256), 0, c.st, (const char*)g, (const char*)rows, inv, w,
+  int waves = LP == 64 ? (int)((c.row_bytes + 1024 * NV - 1) / (1024 * NV)) : 4;
+  if (waves > kGradWaves) waves = kGradWaves;
+  const int64_t blocks = LP == 64 ? c.T : (((int64_t)c.T * LP + 63) / 64 + 3) / 4;
+  hipLaunchKernelGGL((k_combine_grad<DT, K, LP, NV>), dim3((unsigned)blocks), dim3(waves * 64), 0, c.st, (const char*)g, (const char*)rows, inv, w,
                      (char*)grad_rows, grad_w, c.T, c.k, c.R, c.row_bytes);
   return hipGetLastError();
 }
-// Four wavefronts take a token, so that its pieces are requested together.  us, one wavefront a token with 1 / 2 / 4 pieces a lane, four
-// with 1 / 2: 32768 tokens of 4096 columns, k = 2 284 / 287 / 268, 238 / 228; 16384 of 2048, k = 4 127 / 120 / 113, 102 / 110; 4096 of 3584, k = 8
-// 98 / 99 / 99, 93 / 92; 128 of 4096, k = 2 6.4 / 6.1 / 5.6, 3.5 / 3.5; 16384 of 600, k = 2 25 / 24 / 25, 23 / 28.
 template <int DT, int K>
 hipError_t combine_grad_k(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
   switch (lanes_of(c)) {
-    case 8: return combine_grad_as<DT, K, 8, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
-    case 32: return combine_grad_as<DT, K, 32, 1, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+    case 8: return combine_grad_as<DT, K, 8, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+    case 32: return combine_grad_as<DT, K, 32, 1>(c, g, rows, inv, w, grad_rows, grad_w);
     default:
-      if (c.row_bytes <= 4 * 1024) return combine_grad_as<DT, K, 64, 1, 4>(c, g, rows, inv, w, grad_rows, grad_w);
-      return combine_grad_as<DT, K, 64, 2, 4>(c, g, rows, inv, w, grad_rows, grad_w);
+      if (c.row_bytes <= kGradWaves * 1024) return combine_grad_as<DT, K, 64, 1>(c, g, rows, inv, w, grad_rows, grad_w);
+      return combine_grad_as<DT, K, 64, 2>(c, g, rows, inv, w, grad_rows, grad_w);
   }
 }
 template <int DT>
