@@ -1,5 +1,8 @@
 """The operators around the experts together: a block's forward and backward as a program runs them, against automatic
-differentiation in 64 bits and against differences; captured in a graph; on another stream; what the binding refuses."""
+differentiation in 64 bits and against differences; captured in a graph; on another stream; what the binding refuses.
+
+Streams share a few hardware queues in the order in which they come into use.  The tests of ready flags need one that
+runs beside the default stream, so this file, which uses several, comes after theirs."""
 import pytest
 import torch
 
