@@ -56,6 +56,43 @@ __device__ __forceinline__ void scan_buckets(const int32_t* count, int32_t* firs
   }
 }
 
+// Up to RUNS * 64 pairs in one workgroup: a run of 64 pairs a wavefront, ranks inside it by ballots, prefix sums over the runs.  us for 32
+// pairs with one run / as one of the chunks below 2.2 / 2.8, 192 with four 2.3 / 2.9, 1024 with sixteen 3.0 / 3.1.
+template <int RUNS>
+__global__ __launch_bounds__(RUNS * 64) void k_sort_one(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ offsets,
+                                                        int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
+  constexpr int kThreads = RUNS * 64;
+  __shared__ int32_t run_cnt[RUNS][kBuckets];
+  __shared__ int32_t count[kBuckets], first[kBuckets];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = threadIdx.x;
+  const int e = q < R ? bucket_of(ids, q, E) : -1;
+  for (int i = threadIdx.x; i < RUNS * kBuckets; i += kThreads) (&run_cnt[0][0])[i] = 0;
+  __syncthreads();
+  const uint64_t same = same_bucket(e, e >= 0), below = same & ((1ull << lane) - 1ull);
+  const int rank = __popcll(below);
+  if (e >= 0 && below == 0) run_cnt[wave][e] = __popcll(same);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBuckets; i += kThreads) {
+    int acc = 0;
+#pragma unroll
+    for (int r = 0; r < RUNS; r++) {
+      const int c = run_cnt[r][i];
+      run_cnt[r][i] = acc;
+      acc += c;
+    }
+    count[i] = acc;
+  }
+  __syncthreads();
+  scan_buckets(count, first);
+  __syncthreads();
+  if (e >= 0) {
+    const int pos = first[e] + run_cnt[wave][e] + rank;
+    perm[pos] = e < E ? q : -1;
+    inv[q] = e < E ? pos : -1;
+  }
+  for (int i = threadIdx.x; i <= E; i += kThreads) offsets[i] = first[i];
+}
+
 // Pairs of each bucket in each chunk.
 __global__ __launch_bounds__(1024) void k_sort_hist(const int32_t* __restrict__ ids, int R, int E, int32_t* __restrict__ hist) {
   __shared__ int32_t count[kBuckets];
@@ -122,22 +159,18 @@ __global__ __launch_bounds__(1024) void k_sort_scatter(const int32_t* __restrict
   }
   __syncthreads();
   if constexpr (OWN) {
-    if (n_chunks > 1) {
-      const int copy = lane & (kCopies - 1), fours = R / 4;
-      auto one = [&](int id, int later) { atomicAdd(&own[later][copy][(unsigned)id < (unsigned)E ? id : E], 1); };
+    const int copy = lane & (kCopies - 1), fours = R / 4;
+    auto one = [&](int id, int later) { atomicAdd(&own[later][copy][(unsigned)id < (unsigned)E ? id : E], 1); };
 #pragma unroll 4
-      for (int i = threadIdx.x; i < fours; i += 1024) {
-        const int4 v = ((const int4*)ids)[i];
-        const int later = i * 4 >= (int)blockIdx.x * kSortChunk;   // (four pairs never lie in two chunks)
-        one(v.x, later);
-        one(v.y, later);
-        one(v.z, later);
-        one(v.w, later);
-      }
-      if (fours * 4 + (int)threadIdx.x < R) one(ids[fours * 4 + threadIdx.x], 1);   // up to three, in the last chunk
-    } else if (e >= 0) {
-      atomicAdd(&own[1][lane & (kCopies - 1)][e], 1);
+    for (int i = threadIdx.x; i < fours; i += 1024) {
+      const int4 v = ((const int4*)ids)[i];
+      const int later = i * 4 >= (int)blockIdx.x * kSortChunk;   // (four pairs never lie in two chunks)
+      one(v.x, later);
+      one(v.y, later);
+      one(v.z, later);
+      one(v.w, later);
     }
+    if (fours * 4 + (int)threadIdx.x < R) one(ids[fours * 4 + threadIdx.x], 1);   // up to three, in the last chunk
   } else if (total == nullptr) {
     const int parts = n <= 1024 / 16 ? 16 : n <= 1024 / 8 ? 8 : 3;
     const int b = threadIdx.x % n, part = threadIdx.x / n;
@@ -596,6 +629,11 @@ int moe_sort_tokens(const int32_t* topk_ids, int32_t T, int32_t E, int32_t k, in
   if (!apart({{expert_offsets, (size_t)(E + 1) * 4}, {perm, pairs}, {inv_perm, pairs}, {workspace, need}}, {{topk_ids, pairs}})) return MOE_ERR_INVALID_ARG;
   int32_t* hist = (int32_t*)workspace;
   const int n_chunks = n_chunks_of(R);
+  if (R <= kSortChunk) {
+    auto kernel = R <= 64 ? k_sort_one<1> : R <= 256 ? k_sort_one<4> : k_sort_one<16>;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(R <= 64 ? 64 : R <= 256 ? 256 : 1024), 0, st, topk_ids, R, E, expert_offsets, perm, inv_perm);
+    return status_of(hipGetLastError());
+  }
   if (n_chunks <= kSortOwnCounts) {
     hipLaunchKernelGGL(k_sort_scatter<true>, dim3(n_chunks), dim3(1024), 0, st, topk_ids, R, E, nullptr, n_chunks, nullptr, expert_offsets, perm, inv_perm);
     return status_of(hipGetLastError());

@@ -19,7 +19,7 @@ def _sort(moe, ids, E):
 
 
 @pytest.mark.parametrize("T,E,k,dropped", [
-    (1, 1, 1, 0.0), (1, 256, 64, 0.0), (3, 4, 2, 0.5), (16, 8, 2, 0.0), (31, 200, 33, 0.1), (512, 8, 2, 0.0), (513, 8, 2, 0.2), (2048, 64, 2, 0.0),
+    (1, 1, 1, 0.0), (1, 256, 64, 0.0), (3, 4, 2, 0.5), (16, 8, 2, 0.0), (31, 200, 33, 0.1), (13, 8, 5, 0.1), (128, 8, 2, 0.0), (43, 8, 6, 0.1), (512, 8, 2, 0.0), (513, 8, 2, 0.2), (2048, 64, 2, 0.0),
     (2049, 64, 2, 0.3), (1000, 63, 8, 0.0), (1000, 64, 8, 0.1), (1000, 127, 8, 0.1), (1000, 128, 8, 0.0), (4096, 16, 8, 0.1), (4097, 16, 8, 0.1), (8000, 100, 8, 0.1),
     (5000, 256, 8, 0.1),
     (65536, 8, 8, 0.05), (70001, 8, 8, 0.05), (262144 + 77, 256, 8, 0.01)])
