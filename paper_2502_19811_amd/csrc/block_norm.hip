@@ -26,6 +26,61 @@ struct NormParams {
   float scale, eps, inv_h;
 };
 
+struct NormColumnParams {
+  const float* part_a;
+  const float* part_b;    // or nullptr
+  const char* gamma;
+  const char* beta;       // or nullptr
+  const char* gate;       // a channel gate, or nullptr
+  float* grad_gamma;      // each or nullptr
+  float* grad_beta;
+  float* grad_gate;
+  int32_t groups, H;      // rows of part_a and part_b, columns
+};
+
+// What becomes of a column's sums.
+template <int DT>
+__device__ __forceinline__ void finish_column(const NormColumnParams& p, int col, float sa, float sb) {
+  auto value = [&](const char* v) -> float {
+    if constexpr (DT == MOE_BF16) return __uint_as_float((uint32_t)((const uint16_t*)v)[col] << 16);
+    else if constexpr (DT == MOE_FP16) return (float)((const _Float16*)v)[col];
+    else return ((const float*)v)[col];
+  };
+  const float gate = p.gate != nullptr ? value(p.gate) : 1.f;
+  if (p.grad_gamma != nullptr) p.grad_gamma[col] = sa * gate;
+  if (p.grad_beta != nullptr) p.grad_beta[col] = sb * gate;
+  if (p.grad_gate != nullptr) p.grad_gate[col] = fmaf(value(p.gamma), sa, p.beta != nullptr ? value(p.beta) * sb : 0.f);
+}
+
+template <int N>
+__device__ __forceinline__ void store_sums(float* to, const float (&v)[N]) {
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int c = 0; c < N; c += 4) *(f32x4_any*)(to + c) = f32x4_any{v[c], v[c + 1], v[c + 2], v[c + 3]};
+}
+// The same for the columns of a piece.
+template <int DT, int N>
+__device__ __forceinline__ void finish_piece(const NormColumnParams& p, uint32_t start, uint32_t row_bytes, float (&sa)[N], float (&sb)[N]) {
+  using V = Row<DT>;
+  const int col = (int)(piece_at(start, row_bytes) / V::kBytes);
+  float gamma[N], beta[N], gate[N], o[N];
+  V::unpack(load_piece(p.gamma, start, row_bytes), gamma);
+  if (p.beta != nullptr) V::unpack(load_piece(p.beta, start, row_bytes), beta);
+  if (p.gate != nullptr) V::unpack(load_piece(p.gate, start, row_bytes), gate);
+  if (p.grad_gate != nullptr) {
+#pragma unroll
+    for (int c = 0; c < N; c++) o[c] = fmaf(gamma[c], sa[c], p.beta != nullptr ? beta[c] * sb[c] : 0.f);
+    store_sums(p.grad_gate + col, o);
+  }
+#pragma unroll
+  for (int c = 0; c < N; c++) {
+    sa[c] *= p.gate != nullptr ? gate[c] : 1.f;
+    sb[c] *= p.gate != nullptr ? gate[c] : 1.f;
+  }
+  if (p.grad_gamma != nullptr) store_sums(p.grad_gamma + col, sa);
+  if (p.grad_beta != nullptr) store_sums(p.grad_beta + col, sb);
+}
+
 struct NormGradParams {
   const char* v;          // the rows that were normed
   const char* g;          // gradient of the outputs
@@ -41,6 +96,7 @@ struct NormGradParams {
   int32_t gate_kind, layer, T, H, groups;
   uint32_t row_bytes;
   float scale, eps, inv_h;
+  NormColumnParams columns;   // one workgroup: it finishes its sums itself
 };
 
 // Workgroups: MW == 1 four wavefronts with a row each, otherwise a row for up to MW wavefronts, as many as the launch has.
@@ -389,18 +445,30 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p
   }
   if (p.part_a == nullptr) return;
   const float scale = MODE == GRAD_BEFORE ? 1.f : p.scale;
-  auto leave = [&](float* part, float (&acc)[NV][N]) {
-    if constexpr (MW > 1) {
+  if constexpr (MW > 1) {
 #pragma unroll
-      for (int i = 0; i < NV; i++) {
-        if (mine.at[i] >= p.row_bytes) continue;
-        const size_t col = (size_t)blockIdx.x * p.H + piece_at(mine.at[i], p.row_bytes) / V::kBytes;
+    for (int i = 0; i < NV; i++) {
+      if (mine.at[i] >= p.row_bytes) continue;
+      const int col = (int)(piece_at(mine.at[i], p.row_bytes) / V::kBytes);
+      float sa[N], sb[N];
 #pragma unroll
-        for (int c = 0; c < N; c++) part[col + c] = acc[i][c] * scale;
+      for (int c = 0; c < N; c++) {
+        sa[c] = acc_a[i][c] * scale;
+        sb[c] = WITH_B ? acc_b[WITH_B ? i : 0][c] * scale : 0.f;
       }
-    } else {
-      // the four groups of the workgroup meet in LDS, a quarter of the columns a wavefront
-      __shared__ float all[4][NV * N][64];
+      if (gridDim.x == 1) {
+        finish_piece<DT>(p.columns, mine.at[i], p.row_bytes, sa, sb);
+      } else {
+        store_sums(p.part_a + (size_t)blockIdx.x * p.H + col, sa);
+        if constexpr (WITH_B) store_sums(p.part_b + (size_t)blockIdx.x * p.H + col, sb);
+      }
+    }
+  } else {
+    // the four groups of the workgroup meet in LDS, a quarter of the columns a wavefront
+    __shared__ float all[4][NV * N][64];
+    constexpr int kMine = NV * N / 4;
+    float a[kMine], b[kMine];
+    auto meet = [&](float (&sum)[kMine], auto& acc) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < NV; i++)
@@ -408,30 +476,28 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p
         for (int c = 0; c < N; c++) all[wave][i * N + c][lane] = acc[i][c];
       __syncthreads();
 #pragma unroll
-      for (int q = 0; q < NV * N / 4; q++) {
-        const int ic = wave * (NV * N / 4) + q;
-        const uint32_t start = (uint32_t)(ic / N * 64 + lane) * 16;
-        if (start >= p.row_bytes) continue;
-        const size_t col = (size_t)blockIdx.x * p.H + piece_at(start, p.row_bytes) / V::kBytes + ic % N;
-        part[col] = ((all[0][ic][lane] + all[1][ic][lane]) + (all[2][ic][lane] + all[3][ic][lane])) * scale;
+      for (int q = 0; q < kMine; q++) {
+        const int ic = wave * kMine + q;
+        sum[q] = ((all[0][ic][lane] + all[1][ic][lane]) + (all[2][ic][lane] + all[3][ic][lane])) * scale;
+      }
+    };
+    meet(a, acc_a);
+    if constexpr (WITH_B) meet(b, acc_b);
+#pragma unroll
+    for (int q = 0; q < kMine; q++) {
+      const int ic = wave * kMine + q;
+      const uint32_t start = (uint32_t)(ic / N * 64 + lane) * 16;
+      if (start >= p.row_bytes) continue;
+      const int col = (int)(piece_at(start, p.row_bytes) / V::kBytes) + ic % N;
+      if (gridDim.x == 1) {
+        finish_column<DT>(p.columns, col, a[q], WITH_B ? b[q] : 0.f);
+      } else {
+        p.part_a[(size_t)blockIdx.x * p.H + col] = a[q];
+        if constexpr (WITH_B) p.part_b[(size_t)blockIdx.x * p.H + col] = b[q];
       }
     }
-  };
-  leave(p.part_a, acc_a);
-  if constexpr (WITH_B) leave(p.part_b, acc_b);
+  }
 }
-
-struct NormColumnParams {
-  const float* part_a;
-  const float* part_b;    // or nullptr
-  const char* gamma;
-  const char* beta;       // or nullptr
-  const char* gate;       // a channel gate, or nullptr
-  float* grad_gamma;      // each or nullptr
-  float* grad_beta;
-  float* grad_gate;
-  int32_t groups, H;      // rows of part_a and part_b, columns
-};
 
 // Column sums over the groups: a workgroup takes 32 columns, 32 threads each, which go down the groups in turn and meet in LDS.
 template <int DT>
@@ -456,15 +522,7 @@ __global__ __launch_bounds__(1024) void k_norm_columns(NormColumnParams p) {
     sa += a[i][c];
     sb += b[i][c];
   }
-  auto value = [&](const char* v) -> float {
-    if constexpr (DT == MOE_BF16) return __uint_as_float((uint32_t)((const uint16_t*)v)[col] << 16);
-    else if constexpr (DT == MOE_FP16) return (float)((const _Float16*)v)[col];
-    else return ((const float*)v)[col];
-  };
-  const float gate = p.gate != nullptr ? value(p.gate) : 1.f;
-  if (p.grad_gamma != nullptr) p.grad_gamma[col] = sa * gate;
-  if (p.grad_beta != nullptr) p.grad_beta[col] = sb * gate;
-  if (p.grad_gate != nullptr) p.grad_gate[col] = value(p.gamma) * sa + (p.beta != nullptr ? value(p.beta) * sb : 0.f);
+  finish_column<DT>(p, col, sa, sb);
 }
 
 namespace {
@@ -486,9 +544,14 @@ RowShape shape_of(uint32_t pieces) {
 // way and leaves few sums of columns to write and read; then as few as have as many rows each.  us for 10000 rows, before the block, sums of
 // columns included: 2049 columns (5 wavefronts of a piece) 1 / 2 / 4 groups a unit 82 / 58 / 53, behind it with a full gate 85 / 63 / 84; 4104
 // columns (5 of two) 1 / 2 85 / 90, 88 / 97; 3584 columns (7 of one) 4096 rows, 292 groups of 14 or 15 rows 36, 256 of 16 rows 31.
+// Few rows are one workgroup's, which finishes the sums itself; us a call, so / with a launch for the sums: 4 rows of 4096 columns 8.6 / 10.6, with a
+// channel gate and a bias 9.6 / 11.7, 8 rows 9.5 / 10.6 and 12.5 / 11.7; one wavefront a row, 32 rows of 1000 columns 10.2 / 11.7, 64 17.7 / 11.9.
+constexpr int kOneWorkgroupNarrow = 32, kOneWorkgroupWide = 4;
 constexpr int kGroups1 = 4096;   // one wavefront a row: us for 30000 rows of 1024 columns with 4096 / 6144 groups 65 / 67
 int groups_of(int T, uint32_t pieces) {
   const RowShape s = shape_of(pieces);
+  const int side = s.waves == 1 ? 4 : 1;   // groups of a workgroup
+  if (T <= (s.waves == 1 ? kOneWorkgroupNarrow : kOneWorkgroupWide)) return T < side ? T : side;
   const int a_unit = (s.nv == 1 ? 14 : 8) / s.waves, most = s.waves == 1 ? kGroups1 : kDefaultCus * (a_unit > 0 ? a_unit : 1);
   if (T <= most) return T;
   const int each = (T + most - 1) / most;
@@ -555,6 +618,7 @@ hipError_t norm_grad_type(int mode, const NormGradParams& p, const NormColumnPar
     if (e != hipSuccess) return e;
   }
   if (!cp.grad_gamma && !cp.grad_beta && !cp.grad_gate) return hipSuccess;
+  if (cp.groups == 1) return hipSuccess;   // the workgroup has done it
   hipLaunchKernelGGL(k_norm_columns<DT>, dim3((unsigned)((cp.H + 31) / 32)), dim3(1024), 0, st, cp);
   return hipGetLastError();
 }
@@ -708,6 +772,7 @@ int moe_norm_before_backward(const void* sum, const void* gamma, const void* gra
   cp.grad_beta = grad_beta;
   cp.groups = workgroups_of(T, pieces_of(p.row_bytes));
   cp.H = H;
+  p.columns = cp;
   return status_of(launch_norm_grad(dtype, GRAD_BEFORE, p, cp, (hipStream_t)hip_stream));
 }
 
@@ -766,6 +831,7 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   cp.groups = workgroups_of(T, pieces_of(p.row_bytes));
   cp.H = H;
   const int mode = full ? GRAD_AFTER_FULL : token ? GRAD_AFTER_TOKEN : GRAD_AFTER;
+  p.columns = cp;
   return status_of(launch_norm_grad(dtype, mode, p, cp, (hipStream_t)hip_stream));
 }
 

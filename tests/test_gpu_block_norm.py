@@ -74,7 +74,7 @@ def test_before(H, dtype):
 @pytest.mark.parametrize("H", WIDTHS)
 def test_gradient_of_before(H, dtype):
     import paper_2502_19811_amd as moe
-    for T, layer in CASES + [(2500, H % 2 == 0), (4099, H % 2 == 1)]:      # 4099: groups of narrow rows that do not fill a workgroup
+    for T, layer in CASES + [(4, True), (31, False), (2500, H % 2 == 0), (4099, H % 2 == 1)]:      # 4099: groups of narrow rows that do not fill a workgroup
         if T > 2000 and H > (4097 if T == 2500 else 1100):
             continue
         print(f"before gradient T {T} H {H} layer {layer} {dtype}", flush=True)
@@ -148,7 +148,7 @@ def test_after(H, dtype):
 @pytest.mark.parametrize("H", WIDTHS)
 def test_gradient_of_after(H, dtype):
     import paper_2502_19811_amd as moe
-    for (T, layer), gate in itertools.product(CASES + [(2500, H % 2 == 1), (4099, H % 2 == 0)], GATES):
+    for (T, layer), gate in itertools.product(CASES + [(4, False), (31, True), (2500, H % 2 == 1), (4099, H % 2 == 0)], GATES):
         if (T > 2000 and (H > (4097 if T == 2500 else 1100) or gate == "none")) or (T == 1 and gate == "none"):
             continue
         print(f"after gradient T {T} H {H} layer {layer} gate {gate} {dtype}", flush=True)
