@@ -147,6 +147,35 @@ def test_the_same_call_gives_the_same_bits(dtype):
             assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("H", [264, 1001, 3584, 4097])
+def test_a_row_does_not_depend_on_the_batch_around_it(H):
+    """The first rows of a batch against a batch of them alone: every result that belongs to a row."""
+    import paper_2502_19811_amd as moe
+    bf, T, k = torch.bfloat16, 5000, 2
+    norm, kind = moe.MOE_NORM_LAYER, moe.MOE_GATE_TOKEN
+    h, u, g, y = (ro.dev((T, H), bf, 100 + i) for i in range(4))
+    gamma, beta, gate = ro.dev((H,), bf, 104), ro.dev((H,), bf, 105), ro.dev((T,), torch.float32, 106)
+    inv = torch.arange(T * k, dtype=torch.int32, device="cuda").reshape(T, k)
+    rows, w = ro.dev((T * k, H), bf, 107), ro.dev((T, k), torch.float32, 108)
+    results = []
+    for n in (T, 3, 33):
+        H1, U, G, Y, GATE, INV, ROWS, W = h[:n], u[:n], g[:n], y[:n], gate[:n].contiguous(), inv[:n], rows[:n * k], w[:n].contiguous()
+        new = lambda: torch.empty((n, H), dtype=bf, device="cuda")  # noqa: E731
+        s, x, out, gr, gu, gy, c = (new() for _ in range(7))
+        grad_rows, grad_w, grad_gate = torch.empty_like(ROWS), torch.empty_like(W), torch.empty_like(GATE)
+        sums, ws = torch.empty(H, device="cuda"), torch.empty(moe.moe_norm_workspace_bytes(n, H), dtype=torch.uint8, device="cuda")
+        moe.moe_norm_before(H1, U, SCALE, gamma, beta, norm, EPS, s, x)
+        moe.moe_norm_before_backward(H1, gamma, G, U, SCALE, norm, EPS, gr, gu, sums, None, ws)
+        moe.moe_norm_after(H1, Y, gamma, beta, GATE, kind, SCALE, norm, EPS, out)
+        moe.moe_norm_after_backward(Y, gamma, beta, GATE, kind, SCALE, G, norm, EPS, gy, sums, None, grad_gate, ws)
+        moe.moe_combine(ROWS, INV, W, c)
+        moe.moe_combine_backward(G, ROWS, INV, W, grad_rows, grad_w)
+        results.append((s, x, gr, gu, out, gy, grad_gate, c, grad_rows, grad_w))
+    for few in results[1:]:
+        for a, b in zip(few, results[0]):
+            assert torch.equal(a, b[:a.shape[0]])
+
+
 def _without_products(b):
     """The operators alone, for a graph and another stream: the experts' results are what they were."""
     m = b.moe
