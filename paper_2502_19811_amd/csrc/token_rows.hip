@@ -415,57 +415,42 @@ __global__ __launch_bounds__(LP == 64 ? kGradWaves * 64 : 256) void k_combine_gr
 }
 
 // The weights of a token are the softmax of its kept logits, so d w_i / d logit_j = w_i (delta_ij - w_j) among them:
-// grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A thread takes 4 experts of a token and reads its
-// slots in groups of K, all of a group at once.
-template <int K>
+// grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A workgroup takes up to 1024 logits of whole tokens,
+// adds the slots in LDS, a thread a token in the order of j, and writes them in one piece.  (Every thread going through its token's slots
+// for 4 experts: 28.4 us for 65536 tokens of 256 experts, k = 8, so 20.7; 32768 of 64, k = 8 6.2 / 4.9; 32768 of 8, k = 2 2.6 / 3.0.)
+constexpr int kGateLogits = 1024;
 __global__ __launch_bounds__(256) void k_route_topk_grad(const int32_t* __restrict__ ids, const float* __restrict__ w,
-                                                         const float* __restrict__ gw, int64_t n_units, int E, int k, int quads,
+                                                         const float* __restrict__ gw, int T, int E, int k, int tokens,
                                                          float* __restrict__ out) {
-  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (unit >= n_units) return;
-  const int t = (int)((uint32_t)unit / (uint32_t)quads);
-  const int e0 = ((int)unit - t * quads) * 4;
-  const size_t first = (size_t)t * k;
-  float o[4] = {0.f, 0.f, 0.f, 0.f};
-  int id[K];
-  float wj[K], gj[K], sum = 0.f;
-  auto read = [&](int j0) {
+  __shared__ float tile[kGateLogits], wj[kGateLogits], gj[kGateLogits];   // (k <= E: no more slots than logits)
+  __shared__ int32_t id[kGateLogits];
+  const int t0 = blockIdx.x * tokens, n = min(tokens, T - t0), tid = threadIdx.x;
+  const size_t slot0 = (size_t)t0 * k;
 #pragma unroll
-    for (int j = 0; j < K; j++) {
-      const bool there = j0 + j < k;
-      id[j] = there ? ids[first + j0 + j] - e0 : -1;
-      wj[j] = there ? w[first + j0 + j] : 0.f;
-      gj[j] = there ? gw[first + j0 + j] : 0.f;
+  for (int i = 0; i < kGateLogits / 256; i++) {
+    const int s = i * 256 + tid;
+    if (s < n * k) {
+      id[s] = ids[slot0 + s];
+      wj[s] = w[slot0 + s];
+      gj[s] = gw[slot0 + s];
     }
-  };
-  auto add = [&]() {
-#pragma unroll
-    for (int j = 0; j < K; j++) {
-      const float d = wj[j] * (gj[j] - sum);
-#pragma unroll
-      for (int c = 0; c < 4; c++) o[c] += id[j] == c ? d : 0.f;
-    }
-  };
-  for (int j0 = 0; j0 < k; j0 += K) {
-    read(j0);
-#pragma unroll
-    for (int j = 0; j < K; j++) sum = fmaf(gj[j], wj[j], sum);
+    tile[s] = 0.f;
   }
-  if (k <= K) {
-    add();
-  } else {
-    for (int j0 = 0; j0 < k; j0 += K) {
-      read(j0);
-      add();
+  __syncthreads();
+  for (int t = tid; t < n; t += 256) {
+    float sum = 0.f;
+    for (int j = 0; j < k; j++) sum = fmaf(gj[t * k + j], wj[t * k + j], sum);
+    for (int j = 0; j < k; j++) {
+      const int e = id[t * k + j];
+      if ((unsigned)e < (unsigned)E) tile[t * E + e] += wj[t * k + j] * (gj[t * k + j] - sum);
     }
   }
-  float* dst = out + (size_t)t * E + e0;
-  if (E % 4 == 0) {
-    *(float4*)dst = make_float4(o[0], o[1], o[2], o[3]);
-  } else {
+  __syncthreads();
+  float* dst = out + (size_t)t0 * E;
 #pragma unroll
-    for (int c = 0; c < 4; c++)
-      if (e0 + c < E) dst[c] = o[c];
+  for (int i = 0; i < kGateLogits / 256; i++) {
+    const int s = i * 256 + tid;
+    if (s < n * E) dst[s] = tile[s];
   }
 }
 
@@ -703,11 +688,9 @@ int moe_route_topk_backward(const int32_t* topk_ids, const float* topk_weights, 
   if (!aligned16(topk_ids) || !aligned16(topk_weights) || !aligned16(grad_weights) || !aligned16(grad_logits)) return MOE_ERR_INVALID_ARG;
   const size_t pairs = (size_t)T * k * 4;
   if (!apart({{grad_logits, (size_t)T * E * 4}}, {{topk_ids, pairs}, {topk_weights, pairs}, {grad_weights, pairs}})) return MOE_ERR_INVALID_ARG;
-  const int quads = (E + 3) / 4;
-  const int64_t n_units = (int64_t)T * quads;
-  auto kernel = k <= 2 ? k_route_topk_grad<2> : k <= 4 ? k_route_topk_grad<4> : k_route_topk_grad<8>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((n_units + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, topk_ids, topk_weights, grad_weights,
-                     n_units, E, k, quads, grad_logits);
+  const int tokens = kGateLogits / E;
+  hipLaunchKernelGGL(k_route_topk_grad, dim3((unsigned)((T + tokens - 1) / tokens)), dim3(256), 0, (hipStream_t)hip_stream, topk_ids, topk_weights,
+                     grad_weights, T, E, k, tokens, grad_logits);
   return status_of(hipGetLastError());
 }
 
