@@ -22,6 +22,7 @@ struct NormParams {
   char* sum;              // before: the new stream or nullptr
   char* out;
   int32_t gate_kind, layer, T;
+  int32_t in_place;       // an output lies in the place of an input
   uint32_t row_bytes;
   float scale, eps, inv_h;
 };
@@ -94,6 +95,7 @@ struct NormGradParams {
   float* part_a;          // [workgroups][H] sums over the rows of a workgroup, or nullptr
   float* part_b;
   int32_t gate_kind, layer, T, H, groups;
+  int32_t in_place;       // an output lies in the place of an input
   uint32_t row_bytes;
   float scale, eps, inv_h;
   NormColumnParams columns;   // one workgroup: it finishes its sums itself
@@ -114,8 +116,8 @@ __device__ __forceinline__ void clear_absent(RowSums<MW>& sums) {
   }
 }
 // Sums over the wavefronts of a row, in every lane of them.
-// ragged: the last pieces of a row share bytes, perhaps across two wavefronts, and an output may lie in an input's place: what
-// was requested has to be there before any wavefront goes on to its stores.
+// ragged: the last pieces of a row share bytes, perhaps across two wavefronts, and an output lies in an input's place: what was
+// requested has to be there before any wavefront goes on to its stores.
 template <int MW, int N>
 __device__ __forceinline__ void row_sums(RowSums<MW>& sums, float (&v)[N], int place, bool ragged) {
   if (ragged) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm(NormParams p) {
   __shared__ RowSums<MW> sums;
   clear_absent(sums);
   const size_t row = (size_t)t * p.row_bytes;
-  const bool ragged = !EXACT && p.row_bytes % 16 != 0;
+  const bool ragged = !EXACT && p.in_place && p.row_bytes % 16 != 0;
   const Pieces<DT, MW, NV, EXACT> mine(wave, lane, p.row_bytes);
   u32x4 rv[NV], bv[NV], gv[NV], hv[NV];
   if (!AFTER || p.residual != nullptr)
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p
   const int group = MW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   __shared__ RowSums<MW> sums;
   clear_absent(sums);
-  const bool ragged = !ALL && p.row_bytes % 16 != 0;
+  const bool ragged = !ALL && p.in_place && p.row_bytes % 16 != 0;
   const Pieces<DT, MW, NV, ALL> mine(wave, lane, p.row_bytes);
   float gamma[NV][N];   // with a channel gate multiplied in
   u32x4 beta[NV];
@@ -654,6 +656,13 @@ bool in_place_or_apart(const void* out, std::initializer_list<const void*> ins, 
   return true;
 }
 
+bool in_place(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* out : outs)
+    for (const void* in : ins)
+      if (out && out == in) return true;
+  return false;
+}
+
 int status_of(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 }  // namespace
@@ -683,6 +692,7 @@ int moe_norm_before(const void* residual, const void* update, float residual_sca
   p.beta = (const char*)beta;
   p.sum = (char*)sum;
   p.out = (char*)x;
+  p.in_place = in_place({sum, x}, {residual, update});
   p.layer = norm == MOE_NORM_LAYER;
   p.T = T;
   p.row_bytes = (uint32_t)row_bytes;
@@ -713,6 +723,7 @@ int moe_norm_after(const void* residual, const void* y, const void* gamma, const
   p.gate = (const char*)gate;
   p.gate_kind = gate_kind;
   p.out = (char*)out;
+  p.in_place = in_place({out}, {residual, y, gate});
   p.layer = norm == MOE_NORM_LAYER;
   p.T = T;
   p.row_bytes = (uint32_t)row_bytes;
@@ -754,6 +765,7 @@ int moe_norm_before_backward(const void* sum, const void* gamma, const void* gra
   p.more = (const char*)grad_sum;
   p.grad_v = (char*)grad_residual;
   p.grad_other = (char*)grad_update;
+  p.in_place = in_place({grad_residual, grad_update}, {sum, grad_x, grad_sum});
   p.layer = norm == MOE_NORM_LAYER;
   p.T = T;
   p.H = H;
@@ -808,6 +820,7 @@ int moe_norm_after_backward(const void* y, const void* gamma, const void* beta, 
   p.gate_kind = gate_kind;
   p.grad_v = (char*)grad_y;
   p.grad_other = full ? (char*)grad_gate : nullptr;
+  p.in_place = in_place({grad_y, grad_full}, {y, grad_out, full_gate});
   p.grad_token_gate = token ? (float*)grad_gate : nullptr;
   p.layer = norm == MOE_NORM_LAYER;
   p.T = T;
