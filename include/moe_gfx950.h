@@ -298,7 +298,7 @@ int moe_last_device_status(const moe_plan_t *plan, const void *workspace, void *
  * block, and the gradients of these and of the gate.  Rows are bf16, fp16 or fp32 (moe_dtype_t); sums over them are fp32, each
  * result is rounded once.  The same call gives the same bits every time, and a token's or row's bits depend neither on the batch around
  * it nor on which optional results are wanted.  No plan, and no state between calls: workspaces are
- * scratch, and calls that may overlap in time need one each.
+ * scratch, that of a larger batch does for a smaller one, and calls that may overlap in time need one each.
  * Supported: T >= 0; 8 <= H <= 65536 (norms: 16384), odd H included; 1 <= k <= 64, E <= 256, T*k < 2^24 (norms: T < 2^24),
  * T*H*(bytes of an element) < 2^35; anything else is MOE_ERR_UNSUPPORTED.  Row offsets are 64-bit.  With T = 0 the row pointers may be
  * NULL, and what sums over tokens is written as zeros.  Outputs and workspaces that share bytes with inputs or each other, except

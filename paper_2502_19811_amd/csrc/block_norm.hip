@@ -550,19 +550,29 @@ RowShape shape_of(uint32_t pieces) {
 // channel gate and a bias 9.6 / 11.7, 8 rows 9.5 / 10.6 and 12.5 / 11.7; one wavefront a row, 32 rows of 1000 columns 10.2 / 11.7, 64 17.7 / 11.9.
 constexpr int kOneWorkgroupNarrow = 32, kOneWorkgroupWide = 4;
 constexpr int kGroups1 = 4096;   // one wavefront a row: us for 30000 rows of 1024 columns with 4096 / 6144 groups 65 / 67
-int groups_of(int T, uint32_t pieces) {
+int most_groups(uint32_t pieces) {
   const RowShape s = shape_of(pieces);
-  const int side = s.waves == 1 ? 4 : 1;   // groups of a workgroup
-  if (T <= (s.waves == 1 ? kOneWorkgroupNarrow : kOneWorkgroupWide)) return T < side ? T : side;
-  const int a_unit = (s.nv == 1 ? 14 : 8) / s.waves, most = s.waves == 1 ? kGroups1 : kDefaultCus * (a_unit > 0 ? a_unit : 1);
+  const int a_unit = (s.nv == 1 ? 14 : 8) / s.waves;
+  return s.waves == 1 ? kGroups1 : kDefaultCus * (a_unit > 0 ? a_unit : 1);
+}
+int groups_of(int T, uint32_t pieces) {
+  const bool narrow = shape_of(pieces).waves == 1;
+  const int side = narrow ? 4 : 1, most = most_groups(pieces);   // side: groups of a workgroup
+  if (T <= (narrow ? kOneWorkgroupNarrow : kOneWorkgroupWide)) return T < side ? T : side;
   if (T <= most) return T;
   const int each = (T + most - 1) / most;
   return (T + each - 1) / each;
 }
-// Workgroups of the gradients, each of which leaves a row of column sums.
+// Workgroups of the gradients, each of which leaves a row of column sums; and the most that this or a smaller batch has, which is what a
+// workspace is for (more rows may come out in fewer groups).
 int workgroups_of(int T, uint32_t pieces) {
   const int groups = groups_of(T, pieces);
   return shape_of(pieces).waves == 1 ? (groups + 3) / 4 : groups;
+}
+int most_workgroups(int T, uint32_t pieces) {
+  const bool narrow = shape_of(pieces).waves == 1;
+  const int most = most_groups(pieces), groups = T <= (narrow ? kOneWorkgroupNarrow : kOneWorkgroupWide) ? 1 : T < most ? T : most;
+  return narrow ? (groups + 3) / 4 : groups;
 }
 
 template <int DT, bool AFTER, int MW, int NV>
@@ -735,9 +745,9 @@ int moe_norm_after(const void* residual, const void* y, const void* gamma, const
 
 size_t moe_norm_workspace_bytes(int32_t T, int32_t H) {
   if (norm_shape(T, H) != MOE_OK) return 0;
-  const int two = workgroups_of(T, pieces_of((uint32_t)H * 2)), four = workgroups_of(T, pieces_of((uint32_t)H * 4));
+  const int two = most_workgroups(T, pieces_of((uint32_t)H * 2)), four = most_workgroups(T, pieces_of((uint32_t)H * 4));
   const size_t rows = two > four ? two : four;
-  return 2 * (rows > 0 ? rows : 1) * (size_t)H * 4;
+  return 2 * rows * (size_t)H * 4;
 }
 
 int moe_norm_before_backward(const void* sum, const void* gamma, const void* grad_x, const void* grad_sum, float residual_scale,

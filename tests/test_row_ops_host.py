@@ -147,3 +147,11 @@ def test_workspace_sizes():
     assert sizes[-1] <= 2 * 2048 * 4096 * 4                                           # bounded, however many tokens
     for bad in ((-1, 256), (1, 0), (1, 7), (1, 16385), (1 << 24, 256)):
         assert moe.moe_norm_workspace_bytes(*bad) == 0
+
+
+@pytest.mark.parametrize("H", [8, 300, 1000, 2049, 3584, 4096, 4104, 8192, 16384])
+def test_a_workspace_of_a_batch_does_for_smaller_ones(H):
+    sizes = [moe.moe_norm_workspace_bytes(T, H) for T in [*range(1300), *range(1300, 9000, 37)]]
+    assert sizes == sorted(sizes)
+    sizes = [moe.moe_sort_workspace_bytes(T, 64, 4) for T in range(0, 9000, 37)]
+    assert sizes == sorted(sizes)
