@@ -47,7 +47,11 @@ template <> struct Row<MOE_FP16> {
     u32x4 v;
 #pragma unroll
     for (int c = 0; c < 4; c++) {
-      const f16x2 pr = {(_Float16)f[2 * c], (_Float16)f[2 * c + 1]};
+      // The conversion stays apart from what computed the value: where the compiler joins it to a fused operation, the sum is rounded
+      // to 16 bits at once and not to 32 before, and whether it does depends on the code around.
+      float lo = f[2 * c], hi = f[2 * c + 1];
+      asm("" : "+v"(lo), "+v"(hi));
+      const f16x2 pr = {(_Float16)lo, (_Float16)hi};
       v[c] = __builtin_bit_cast(uint32_t, pr);
     }
     return v;

@@ -191,6 +191,10 @@ def test_gradient_of_after(H, dtype):
         a, b, c = y.clone(), g.clone(), h.clone() if h is not None else None
         moe.moe_norm_after_backward(a, gamma, beta, c, kind, scale, b, norm, EPS, b, None, None, c if gate == "full" else None, None)
         assert torch.equal(b, grad_y) and (gate != "full" or torch.equal(c, grad_gate))
+        if gate in ("token", "full"):       # the gate's gradient not wanted
+            again, other = torch.full((H,), 7.0, device="cuda"), torch.empty_like(y)
+            moe.moe_norm_after_backward(y, gamma, beta, h, kind, scale, g, norm, EPS, other, again, None, None, ws)
+            assert torch.equal(again, grad_gamma) and torch.equal(other, grad_y)
         if gate == "channel":
             again = torch.full((H,), 7.0, device="cuda")
             moe.moe_norm_after_backward(y, gamma, beta, h, kind, scale, g, norm, EPS, a, None, None, again, ws)

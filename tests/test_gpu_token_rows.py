@@ -222,6 +222,34 @@ def test_indices_outside_are_no_row(dtype):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+@pytest.mark.parametrize("H", [30001, 65536])
+def test_the_widest_rows(H, dtype):
+    import paper_2502_19811_amd as moe
+    T, k = 7, 3
+    print(f"widest rows H {H} {dtype}", flush=True)
+    _, inv, w = _pairs(T, 8, k, H, 0.2)
+    x, g = ro.dev((T, H), dtype, 11), ro.dev((T, H), dtype, 12)
+    rows, check = ro.guarded((T * k, H), dtype, 7.0)
+    moe.moe_dispatch(x, inv, rows)
+    kept = inv >= 0
+    at, tok = inv[kept].long(), torch.nonzero(kept)[:, 0]
+    assert torch.equal(rows[at], x[tok])
+    check()
+    out = torch.empty_like(x)
+    moe.moe_combine(rows, inv, w, out)
+    ref, size = ro.combine(rows, inv, w)
+    ro.close(out, ref, (k + 1) * ro.STEP32 * size, "combine")
+    grad_rows, check = ro.guarded((T * k, H), dtype, 7.0)
+    grad_w = torch.empty((T, k), device="cuda")
+    moe.moe_combine_backward(g, rows, inv, w, grad_rows, grad_w)
+    ref = g[tok].double() * w[kept].double()[:, None]
+    ro.close(grad_rows[at], ref, ro.STEP32 * ref.abs(), "grad_rows")
+    products = g[tok].double() * rows[at].double()
+    ro.close(grad_w[kept], products.sum(dim=1), (H / 8 + 24) * ro.STEP32 * products.abs().sum(dim=1), "grad_weights")
+    check()
+
+
 @pytest.mark.parametrize("dtype", ro.DTYPES, ids=str)
 def test_no_tokens(dtype):
     import paper_2502_19811_amd as moe
