@@ -9,6 +9,7 @@ import ctypes as C
 import os
 from typing import Optional, Sequence
 
+MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED = -1, -4
 MOE_ACT_GELU = 0
 MOE_ACT_SWIGLU = 1
 MOE_BF16, MOE_FP16, MOE_FP32 = 0, 1, 2
@@ -144,6 +145,13 @@ def _check(status: int, where: str) -> None:
         raise MoEError(status, where)
 
 
+# The C calls take sizes as 32-bit integers, and ctypes cuts what is longer without a word: 2**32 rows would be none.  So sizes are
+# tested first, where calls are short those of a call together: (a | b | ...) >> 31 is 0 if all of them fit and none is negative.
+def _check_int32(where: str, *values: int) -> None:
+    if any(not -1 << 31 <= v < 1 << 31 for v in values):
+        raise MoEError(MOE_ERR_UNSUPPORTED, where)
+
+
 def moe_status_string(status: int) -> str:
     return load_library().moe_status_string(status).decode()
 
@@ -151,6 +159,7 @@ def moe_status_string(status: int) -> str:
 def moe_plan_create(T: int, H: int, F: int, E: int, k: int, S: int, act: int, seg_offsets: Sequence[int]) -> int:
     """Returns the plan handle.  seg_offsets: S+1 host integers."""
     lib = load_library()
+    _check_int32("moe_plan_create", T, H, F, E, k, S, act, *seg_offsets)
     shape = MoEShape(T, H, F, E, k, S, act)
     seg = (C.c_int32 * (S + 1))(*[int(v) for v in seg_offsets])
     handle = C.c_void_p()
@@ -186,6 +195,8 @@ def moe_receive_buffer_bytes(M: int, N: int) -> int:
 
 def moe_route_topk(logits, k: int, topk_ids, topk_weights, stream=None) -> None:
     T, E = logits.shape
+    if (T | E | k) >> 31:
+        _check_int32("moe_route_topk", T, E, k)
     _check(load_library().moe_route_topk(_ptr(logits), T, E, k, _ptr(topk_ids), _ptr(topk_weights), _stream(stream)),
            "moe_route_topk")
 
@@ -327,8 +338,8 @@ class _Call:
         else:
             self.refuse()
 
-    def refuse(self):
-        raise MoEError(-1, self.where)
+    def refuse(self, status: int = MOE_ERR_INVALID_ARG):
+        raise MoEError(status, self.where)
 
     def arg(self, t, dtype, shape) -> int:
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
@@ -342,13 +353,19 @@ class _Call:
         """(shape, type, its number) of a tensor of rows."""
         if t.dim() != 2 or t.dtype not in _DTYPES:
             self.refuse()
-        return t.shape, t.dtype, _DTYPES[t.dtype]
+        T, H = shape = t.shape
+        if (T | H) >> 31:
+            self.refuse(MOE_ERR_UNSUPPORTED)
+        return shape, t.dtype, _DTYPES[t.dtype]
 
     def pairs(self, t):
         """(T, k) of a tensor of pairs."""
         if t.dim() != 2:
             self.refuse()
-        return t.shape
+        T, k = shape = t.shape
+        if (T | k) >> 31:
+            self.refuse(MOE_ERR_UNSUPPORTED)
+        return shape
 
     def workspace(self, t):
         if t is None:
@@ -361,6 +378,8 @@ class _Call:
 
 
 def moe_sort_workspace_bytes(T: int, E: int, k: int) -> int:
+    if (T | E | k) >> 31:      # (negative ones, too: no such shape)
+        return 0
     return load_library().moe_sort_workspace_bytes(T, E, k)
 
 
@@ -368,6 +387,8 @@ def moe_sort_tokens(topk_ids, E: int, expert_offsets, perm, inv_perm, workspace,
     """topk_ids int32 [T,k] -> expert_offsets int32 [E+1], perm int32 [T*k], inv_perm int32 [T,k]; workspace uint8."""
     c = _Call("moe_sort_tokens", stream)
     T, k = pairs = c.pairs(topk_ids)
+    if E >> 31:
+        c.refuse(MOE_ERR_INVALID_ARG if E < 0 else MOE_ERR_UNSUPPORTED)
     c.done(load_library().moe_sort_tokens(
         c.arg(topk_ids, _INT32, pairs), T, E, k, c.arg(expert_offsets, _INT32, (E + 1,)), c.arg(perm, _INT32, (T * k,)),
         c.arg(inv_perm, _INT32, pairs), *c.workspace(workspace), c.stream))
@@ -421,6 +442,8 @@ def moe_route_topk_backward(topk_ids, topk_weights, grad_weights, grad_logits, s
 
 
 def moe_norm_workspace_bytes(T: int, H: int) -> int:
+    if (T | H) >> 31:
+        return 0
     return load_library().moe_norm_workspace_bytes(T, H)
 
 
@@ -429,6 +452,8 @@ def moe_norm_before(residual, update, residual_scale: float, gamma, beta, norm: 
     c = _Call("moe_norm_before", stream)
     s, t, dtype = c.rows(residual)
     T, H = s
+    if norm >> 31:
+        c.refuse()
     c.done(load_library().moe_norm_before(
         c.arg(residual, t, s), c.opt(update, t, s), residual_scale, c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), norm, eps, T, H, dtype,
         c.opt(sum, t, s), c.arg(x, t, s), c.stream))
@@ -440,6 +465,8 @@ def moe_norm_before_backward(sum, gamma, grad_x, grad_sum, residual_scale: float
     c = _Call("moe_norm_before_backward", stream)
     s, t, dtype = c.rows(sum)
     T, H = s
+    if norm >> 31:
+        c.refuse()
     c.done(load_library().moe_norm_before_backward(
         c.arg(sum, t, s), c.arg(gamma, t, (H,)), c.arg(grad_x, t, s), c.opt(grad_sum, t, s), residual_scale, norm, eps, T, H, dtype,
         c.arg(grad_residual, t, s), c.opt(grad_update, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),
@@ -461,6 +488,8 @@ def moe_norm_after(residual, y, gamma, beta, gate, gate_kind: int, residual_scal
     c = _Call("moe_norm_after", stream)
     s, t, dtype = c.rows(y)
     T, H = s
+    if (norm | gate_kind) >> 31:
+        c.refuse()
     c.done(load_library().moe_norm_after(
         c.opt(residual, t, s), c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind,
         residual_scale, norm, eps, T, H, dtype, c.arg(out, t, s), c.stream))
@@ -472,6 +501,8 @@ def moe_norm_after_backward(y, gamma, beta, gate, gate_kind: int, residual_scale
     c = _Call("moe_norm_after_backward", stream)
     s, t, dtype = c.rows(y)
     T, H = s
+    if (norm | gate_kind) >> 31:
+        c.refuse()
     c.done(load_library().moe_norm_after_backward(
         c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind, residual_scale,
         c.arg(grad_out, t, s), norm, eps, T, H, dtype, c.arg(grad_y, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),

@@ -1,0 +1,111 @@
+"""What the binding does before any launch, without a GPU: tensors without memory stand in for those on the device."""
+import pytest
+import torch
+
+import paper_2502_19811_amd as moe
+from paper_2502_19811_amd import binding
+
+INVALID, UNSUPPORTED = -1, -4
+HUGE = [1 << 31, 1 << 32, (1 << 32) + 8, 1 << 40]      # 32 bits make a negative number, none, 8, none out of them
+
+
+@pytest.fixture
+def no_device(monkeypatch):
+    """Calls go through the binding with tensors that are on no device (their device is -1)."""
+    monkeypatch.setattr(binding, "_first_call", lambda: None)
+    monkeypatch.setattr(binding, "_INT32", torch.int32)
+    monkeypatch.setattr(binding, "_FLOAT32", torch.float32)
+    monkeypatch.setattr(binding, "_UINT8", torch.uint8)
+    monkeypatch.setattr(binding, "_current_device", lambda: -1)
+    monkeypatch.setattr(binding, "_raw_stream", lambda device: None)
+    monkeypatch.setattr(binding, "_stream", lambda stream: None)
+    for t, number in ((torch.bfloat16, moe.MOE_BF16), (torch.float16, moe.MOE_FP16), (torch.float32, moe.MOE_FP32)):
+        monkeypatch.setitem(binding._DTYPES, t, number)
+
+
+def _t(*shape, dtype=torch.bfloat16):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+def _i(*shape):
+    return _t(*shape, dtype=torch.int32)
+
+
+def _f(*shape):
+    return _t(*shape, dtype=torch.float32)
+
+
+def _calls(T=0, H=64, E=8, k=2, norm=0, kind=0):
+    """Every call with these sizes; without tokens nothing is launched and no pointer is needed but a gradient's gamma."""
+    ws = _t(1 << 20, dtype=torch.uint8)
+    rows, all_rows, pairs = _t(T, H), _t(T * k, H), (T, k)
+    gate = None
+    return {
+        "moe_route_topk": lambda: moe.moe_route_topk(_f(T, E), k, _i(*pairs), _f(*pairs)),
+        "moe_sort_tokens": lambda: moe.moe_sort_tokens(_i(*pairs), E, _i(E + 1), _i(T * k), _i(*pairs), ws),
+        "moe_dispatch": lambda: moe.moe_dispatch(rows, _i(*pairs), all_rows),
+        "moe_dispatch_backward": lambda: moe.moe_dispatch_backward(all_rows, _i(*pairs), rows),
+        "moe_combine": lambda: moe.moe_combine(all_rows, _i(*pairs), _f(*pairs), rows),
+        "moe_combine_backward": lambda: moe.moe_combine_backward(rows, all_rows, _i(*pairs), _f(*pairs), all_rows, _f(*pairs)),
+        "moe_route_topk_backward": lambda: moe.moe_route_topk_backward(_i(*pairs), _f(*pairs), _f(*pairs), _f(T, E)),
+        "moe_norm_before": lambda: moe.moe_norm_before(rows, None, 1.0, _t(H), None, norm, 1e-5, None, rows),
+        "moe_norm_before_backward": lambda: moe.moe_norm_before_backward(rows, _t(H), rows, None, 1.0, norm, 1e-5, rows, None, None, None, None),
+        "moe_norm_after": lambda: moe.moe_norm_after(None, rows, _t(H), None, gate, kind, 1.0, norm, 1e-5, rows),
+        "moe_norm_after_backward": lambda: moe.moe_norm_after_backward(rows, _t(H), None, gate, kind, 1.0, rows, norm, 1e-5, rows, None, None,
+                                                                       None, None),
+    }
+
+
+ROWS = ["moe_dispatch", "moe_dispatch_backward", "moe_combine", "moe_combine_backward"]
+NORMS = ["moe_norm_before", "moe_norm_before_backward", "moe_norm_after", "moe_norm_after_backward"]
+SIZES = [(name, "T") for name in _calls()] + [(name, "H") for name in ROWS + NORMS] + \
+        [(name, "k") for name in ROWS + ["moe_route_topk", "moe_sort_tokens", "moe_route_topk_backward"]] + \
+        [(name, "E") for name in ("moe_route_topk", "moe_sort_tokens", "moe_route_topk_backward")]
+
+
+@pytest.mark.parametrize("value", HUGE)
+@pytest.mark.parametrize("name,size", SIZES)
+def test_sizes_beyond_32_bits_are_refused(no_device, name, size, value):
+    with pytest.raises(moe.MoEError) as error:
+        _calls(**{size: value})[name]()
+    assert error.value.status == UNSUPPORTED
+
+
+@pytest.mark.parametrize("value", [*HUGE, 2, -1, -(1 << 32)])
+@pytest.mark.parametrize("name", NORMS)
+def test_norms_that_there_are_not(no_device, name, value):
+    with pytest.raises(moe.MoEError) as error:
+        _calls(norm=value)[name]()
+    assert error.value.status == INVALID
+
+
+@pytest.mark.parametrize("value", [*HUGE, 4, -1, -(1 << 32)])
+@pytest.mark.parametrize("name", NORMS[2:])
+def test_gates_that_there_are_not(no_device, name, value):
+    with pytest.raises(moe.MoEError) as error:
+        _calls(kind=value)[name]()
+    assert error.value.status == INVALID
+
+
+def test_negative_numbers_of_experts(no_device):
+    for E in (-1, -(1 << 32)):
+        with pytest.raises(moe.MoEError) as error:
+            moe.moe_sort_tokens(_i(4, 2), E, _i(8), _i(8), _i(4, 2), None)
+        assert error.value.status == INVALID
+
+
+@pytest.mark.parametrize("value", [*HUGE, -(1 << 32)])
+def test_workspaces_and_plans_of_sizes_beyond_32_bits(value):
+    for at in range(3):
+        sizes = [8, 8, 2]
+        sizes[at] = value
+        assert moe.moe_sort_workspace_bytes(*sizes) == 0
+    assert moe.moe_norm_workspace_bytes(value, 256) == 0 and moe.moe_norm_workspace_bytes(1, value) == 0
+    good = dict(T=64, H=256, F=256, E=8, k=2, S=1, act=moe.MOE_ACT_SWIGLU, seg_offsets=[0, 64])
+    moe.moe_plan_destroy(moe.moe_plan_create(**good))
+    for name in ("T", "H", "F", "E", "k", "act"):
+        with pytest.raises(moe.MoEError) as error:
+            moe.moe_plan_create(**{**good, name: value})
+        assert error.value.status == UNSUPPORTED
+    with pytest.raises(moe.MoEError):
+        moe.moe_plan_create(**{**good, "seg_offsets": [0, (1 << 32) + 64]})
