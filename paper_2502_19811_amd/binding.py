@@ -315,10 +315,11 @@ _INT32 = _FLOAT32 = _UINT8 = _current_device = _raw_stream = None
 def _first_call() -> None:
     global _INT32, _FLOAT32, _UINT8, _current_device, _raw_stream
     import torch
-    _INT32, _FLOAT32, _UINT8 = torch.int32, torch.float32, torch.uint8
+    _FLOAT32, _UINT8 = torch.float32, torch.uint8
     _current_device = torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _DTYPES.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
+    _INT32 = torch.int32    # last: another thread goes on once this is there
 
 
 class _Call:

@@ -1,4 +1,6 @@
 """What the binding does before any launch, without a GPU: tensors without memory stand in for those on the device."""
+import sys
+
 import pytest
 import torch
 
@@ -109,3 +111,28 @@ def test_workspaces_and_plans_of_sizes_beyond_32_bits(value):
         assert error.value.status == UNSUPPORTED
     with pytest.raises(moe.MoEError):
         moe.moe_plan_create(**{**good, "seg_offsets": [0, (1 << 32) + 64]})
+
+
+def test_the_first_call_of_two_threads(monkeypatch):
+    """Whenever another thread could look, between any two lines of the first call: what it takes for done is done."""
+    names = ["_INT32", "_FLOAT32", "_UINT8", "_current_device", "_raw_stream"]
+    for name in names:
+        monkeypatch.setattr(binding, name, None)
+    monkeypatch.setattr(binding, "_DTYPES", {})
+    looks = []
+
+    def look(frame, event, arg):
+        if frame.f_code is binding._first_call.__code__:
+            if binding._INT32 is not None:       # what _Call looks at
+                looks.append(len(binding._DTYPES) == 3 and all(getattr(binding, name) is not None for name in names))
+            return look
+        return None
+
+    before = sys.gettrace()
+    sys.settrace(look)
+    try:
+        binding._first_call()
+    finally:
+        sys.settrace(before)
+    assert looks and all(looks)
+    assert binding._INT32 is torch.int32
