@@ -45,7 +45,7 @@ struct NormColumnParams {
   int32_t groups, H;      // rows of part_a and part_b, columns
 };
 
-// What becomes of a column's sums.
+// What becomes of a column's sums.  Without rows (groups == 0) they are 0, whatever the factors are.
 template <int DT>
 __device__ __forceinline__ void finish_column(const NormColumnParams& p, int col, float sa, float sb) {
   auto value = [&](const char* v) -> float {
@@ -53,10 +53,11 @@ __device__ __forceinline__ void finish_column(const NormColumnParams& p, int col
     else if constexpr (DT == MOE_FP16) return (float)((const _Float16*)v)[col];
     else return ((const float*)v)[col];
   };
-  const float gate = p.gate != nullptr ? value(p.gate) : 1.f;
+  const bool rows = p.groups > 0;
+  const float gate = p.gate != nullptr && rows ? value(p.gate) : 1.f;
   if (p.grad_gamma != nullptr) p.grad_gamma[col] = sa * gate;
   if (p.grad_beta != nullptr) p.grad_beta[col] = sb * gate;
-  if (p.grad_gate != nullptr) p.grad_gate[col] = fmaf(value(p.gamma), sa, p.beta != nullptr ? value(p.beta) * sb : 0.f);
+  if (p.grad_gate != nullptr) p.grad_gate[col] = rows ? fmaf(value(p.gamma), sa, p.beta != nullptr ? value(p.beta) * sb : 0.f) : 0.f;
 }
 
 template <int N>
