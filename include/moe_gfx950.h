@@ -302,7 +302,8 @@ int moe_last_device_status(const moe_plan_t *plan, const void *workspace, void *
  * Supported: T >= 0; 8 <= H <= 65536 (norms: 16384), odd H included; 1 <= k <= 64, E <= 256, T*k < 2^24 (norms: T < 2^24),
  * T*H*(bytes of an element) < 2^35; anything else is MOE_ERR_UNSUPPORTED.  Row offsets are 64-bit.  With T = 0 the row pointers may be
  * NULL, and what sums over tokens is written as zeros.  Outputs and workspaces that share bytes with inputs or each other, except
- * where said, are MOE_ERR_INVALID_ARG.
+ * where said, are MOE_ERR_INVALID_ARG.  The calls see memory only: a framework that records gradients neither records them nor learns from
+ * them what they overwrite, which the caller (the Python binding, for the versions of torch's tensors) has to tell it.
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef enum { MOE_BF16 = 0, MOE_FP16 = 1, MOE_FP32 = 2 } moe_dtype_t;
 typedef enum { MOE_NORM_RMS = 0, MOE_NORM_LAYER = 1 } moe_norm_t;

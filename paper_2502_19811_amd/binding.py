@@ -2,6 +2,10 @@
 
 Tensor arguments are torch tensors on the GPU (or None where the C call accepts NULL); only their
 data pointers are passed on.  `stream` is a torch.cuda.Stream or None for the current stream.
+
+No call becomes a node of torch's graph of gradients, whatever its tensors require: a program that wants that wraps a call and
+its backward call in a torch.autograd.Function.  What the gate, the layer and the operators around the experts write counts as written
+there, as after an operation in place: a gradient that needs the former values raises an error (replays of a graph do not count).
 """
 from __future__ import annotations
 
@@ -145,6 +149,13 @@ def _check(status: int, where: str) -> None:
         raise MoEError(status, where)
 
 
+def _written(tensors) -> None:
+    """A call has written these: whoever saved them for a gradient is told by their version (0.1 to 0.2 us)."""
+    if _increment_version is None:
+        _first_call()
+    _increment_version(tensors)
+
+
 # The C calls take sizes as 32-bit integers, and ctypes cuts what is longer without a word: 2**32 rows would be none.  So sizes are
 # tested first, where calls are short those of a call together: (a | b | ...) >> 31 is 0 if all of them fit and none is negative.
 def _check_int32(where: str, *values: int) -> None:
@@ -199,6 +210,7 @@ def moe_route_topk(logits, k: int, topk_ids, topk_weights, stream=None) -> None:
         _check_int32("moe_route_topk", T, E, k)
     _check(load_library().moe_route_topk(_ptr(logits), T, E, k, _ptr(topk_ids), _ptr(topk_weights), _stream(stream)),
            "moe_route_topk")
+    _written((topk_ids, topk_weights))
 
 
 def moe_layer_forward(plan: int, x, topk_ids, topk_weights, W1, W2, act: int, out, workspace, seg_ready=None,
@@ -206,6 +218,7 @@ def moe_layer_forward(plan: int, x, topk_ids, topk_weights, W1, W2, act: int, ou
     _check(load_library().moe_layer_forward(plan, _ptr(x), _ptr(topk_ids), _ptr(topk_weights), _ptr(W1), _ptr(W2), act,
                                             _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                             _ptr(seg_ready), ready_epoch, _stream(stream)), "moe_layer_forward")
+    _written((out,))
 
 
 def moe_layer_forward_static(plan: int, x, topk_ids, topk_weights, W1, W2, act: int, out, seg_ready=None,
@@ -214,6 +227,7 @@ def moe_layer_forward_static(plan: int, x, topk_ids, topk_weights, W1, W2, act: 
     _check(load_library().moe_layer_forward_static(plan, _ptr(x), _ptr(topk_ids), _ptr(topk_weights), _ptr(W1), _ptr(W2),
                                                    act, _ptr(out), _ptr(seg_ready), ready_epoch, _stream(stream)),
            "moe_layer_forward_static")
+    _written((out,))
 
 
 def moe_pack_weights(plan: int, W1, W2, W1_packed, W2_packed, stream=None) -> None:
@@ -306,18 +320,20 @@ def moe_probe_copy(dst, src, stream=None) -> float:
 # ---- operators around the experts ----
 # The C calls see addresses only, so what they cannot check is checked here: every tensor has the type and shape its call
 # says, is contiguous, and lies on the current device, as the stream does.  These calls are often a few microseconds of work:
-# checking a tensor takes 0.3 us, and the current stream is asked for by its address (0.1 us; as an object 1.1).
+# checking a tensor takes 0.3 us, and the current stream is asked for by its address (0.1 us; as an object 1.1).  With the test of the
+# sizes and the versions of what is written a call takes 0.2 to 0.35 us more than without.
 
 _DTYPES = {}            # torch's row types -> their numbers, filled at the first call
-_INT32 = _FLOAT32 = _UINT8 = _current_device = _raw_stream = None
+_INT32 = _FLOAT32 = _UINT8 = _current_device = _raw_stream = _increment_version = None
 
 
 def _first_call() -> None:
-    global _INT32, _FLOAT32, _UINT8, _current_device, _raw_stream
+    global _INT32, _FLOAT32, _UINT8, _current_device, _raw_stream, _increment_version
     import torch
     _FLOAT32, _UINT8 = torch.float32, torch.uint8
     _current_device = torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _increment_version = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
     _DTYPES.update({torch.bfloat16: MOE_BF16, torch.float16: MOE_FP16, torch.float32: MOE_FP32})
     _INT32 = torch.int32    # last: another thread goes on once this is there
 
@@ -373,9 +389,14 @@ class _Call:
             return None, 0
         return self.arg(t, _UINT8, (t.numel(),)), t.numel()
 
-    def done(self, status: int) -> None:
+    def done(self, status: int, *written) -> None:
         if status != 0:
             raise MoEError(status, self.where)
+        _increment_version(written)
+
+
+def _given(*tensors):
+    return [t for t in tensors if t is not None]
 
 
 def moe_sort_workspace_bytes(T: int, E: int, k: int) -> int:
@@ -392,7 +413,7 @@ def moe_sort_tokens(topk_ids, E: int, expert_offsets, perm, inv_perm, workspace,
         c.refuse(MOE_ERR_INVALID_ARG if E < 0 else MOE_ERR_UNSUPPORTED)
     c.done(load_library().moe_sort_tokens(
         c.arg(topk_ids, _INT32, pairs), T, E, k, c.arg(expert_offsets, _INT32, (E + 1,)), c.arg(perm, _INT32, (T * k,)),
-        c.arg(inv_perm, _INT32, pairs), *c.workspace(workspace), c.stream))
+        c.arg(inv_perm, _INT32, pairs), *c.workspace(workspace), c.stream), expert_offsets, perm, inv_perm)
 
 
 def moe_dispatch(x, inv_perm, rows, stream=None) -> None:
@@ -400,7 +421,8 @@ def moe_dispatch(x, inv_perm, rows, stream=None) -> None:
     c = _Call("moe_dispatch", stream)
     (T, H), t, dtype = c.rows(x)
     k = c.pairs(inv_perm)[1]
-    c.done(load_library().moe_dispatch(c.arg(x, t, (T, H)), c.arg(inv_perm, _INT32, (T, k)), T, H, k, dtype, c.arg(rows, t, (T * k, H)), c.stream))
+    c.done(load_library().moe_dispatch(c.arg(x, t, (T, H)), c.arg(inv_perm, _INT32, (T, k)), T, H, k, dtype, c.arg(rows, t, (T * k, H)), c.stream),
+           rows)
 
 
 def moe_dispatch_backward(grad_rows, inv_perm, grad_x, stream=None) -> None:
@@ -409,7 +431,7 @@ def moe_dispatch_backward(grad_rows, inv_perm, grad_x, stream=None) -> None:
     (T, H), t, dtype = c.rows(grad_x)
     k = c.pairs(inv_perm)[1]
     c.done(load_library().moe_dispatch_backward(c.arg(grad_rows, t, (T * k, H)), c.arg(inv_perm, _INT32, (T, k)), T, H, k, dtype,
-                                                c.arg(grad_x, t, (T, H)), c.stream))
+                                                c.arg(grad_x, t, (T, H)), c.stream), grad_x)
 
 
 def moe_combine(rows, inv_perm, topk_weights, out, stream=None) -> None:
@@ -418,7 +440,7 @@ def moe_combine(rows, inv_perm, topk_weights, out, stream=None) -> None:
     (T, H), t, dtype = c.rows(out)
     k = c.pairs(inv_perm)[1]
     c.done(load_library().moe_combine(c.arg(rows, t, (T * k, H)), c.arg(inv_perm, _INT32, (T, k)), c.opt(topk_weights, _FLOAT32, (T, k)),
-                                      T, H, k, dtype, c.arg(out, t, (T, H)), c.stream))
+                                      T, H, k, dtype, c.arg(out, t, (T, H)), c.stream), out)
 
 
 def moe_combine_backward(grad_out, rows, inv_perm, topk_weights, grad_rows, grad_weights, stream=None) -> None:
@@ -429,7 +451,8 @@ def moe_combine_backward(grad_out, rows, inv_perm, topk_weights, grad_rows, grad
     pairs, all_rows = (T, k), (T * k, H)
     c.done(load_library().moe_combine_backward(
         c.arg(grad_out, t, (T, H)), c.opt(rows, t, all_rows), c.arg(inv_perm, _INT32, pairs), c.opt(topk_weights, _FLOAT32, pairs),
-        T, H, k, dtype, c.arg(grad_rows, t, all_rows), c.opt(grad_weights, _FLOAT32, pairs), c.stream))
+        T, H, k, dtype, c.arg(grad_rows, t, all_rows), c.opt(grad_weights, _FLOAT32, pairs), c.stream),
+        *((grad_rows,) if grad_weights is None else (grad_rows, grad_weights)))
 
 
 def moe_route_topk_backward(topk_ids, topk_weights, grad_weights, grad_logits, stream=None) -> None:
@@ -439,7 +462,7 @@ def moe_route_topk_backward(topk_ids, topk_weights, grad_weights, grad_logits, s
     E = c.pairs(grad_logits)[1]
     c.done(load_library().moe_route_topk_backward(
         c.arg(topk_ids, _INT32, pairs), c.arg(topk_weights, _FLOAT32, pairs), c.arg(grad_weights, _FLOAT32, pairs), T, E, k,
-        c.arg(grad_logits, _FLOAT32, (T, E)), c.stream))
+        c.arg(grad_logits, _FLOAT32, (T, E)), c.stream), grad_logits)
 
 
 def moe_norm_workspace_bytes(T: int, H: int) -> int:
@@ -457,7 +480,7 @@ def moe_norm_before(residual, update, residual_scale: float, gamma, beta, norm: 
         c.refuse()
     c.done(load_library().moe_norm_before(
         c.arg(residual, t, s), c.opt(update, t, s), residual_scale, c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), norm, eps, T, H, dtype,
-        c.opt(sum, t, s), c.arg(x, t, s), c.stream))
+        c.opt(sum, t, s), c.arg(x, t, s), c.stream), *((x,) if sum is None else (sum, x)))
 
 
 def moe_norm_before_backward(sum, gamma, grad_x, grad_sum, residual_scale: float, norm: int, eps: float, grad_residual, grad_update,
@@ -471,7 +494,7 @@ def moe_norm_before_backward(sum, gamma, grad_x, grad_sum, residual_scale: float
     c.done(load_library().moe_norm_before_backward(
         c.arg(sum, t, s), c.arg(gamma, t, (H,)), c.arg(grad_x, t, s), c.opt(grad_sum, t, s), residual_scale, norm, eps, T, H, dtype,
         c.arg(grad_residual, t, s), c.opt(grad_update, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),
-        *c.workspace(workspace), c.stream))
+        *c.workspace(workspace), c.stream), *_given(grad_residual, grad_update, grad_gamma, grad_beta))
 
 
 def _gate(c: _Call, gate, kind: int, shape, t) -> Optional[int]:
@@ -493,7 +516,7 @@ def moe_norm_after(residual, y, gamma, beta, gate, gate_kind: int, residual_scal
         c.refuse()
     c.done(load_library().moe_norm_after(
         c.opt(residual, t, s), c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind,
-        residual_scale, norm, eps, T, H, dtype, c.arg(out, t, s), c.stream))
+        residual_scale, norm, eps, T, H, dtype, c.arg(out, t, s), c.stream), out)
 
 
 def moe_norm_after_backward(y, gamma, beta, gate, gate_kind: int, residual_scale: float, grad_out, norm: int, eps: float, grad_y,
@@ -507,4 +530,5 @@ def moe_norm_after_backward(y, gamma, beta, gate, gate_kind: int, residual_scale
     c.done(load_library().moe_norm_after_backward(
         c.arg(y, t, s), c.arg(gamma, t, (H,)), c.opt(beta, t, (H,)), _gate(c, gate, gate_kind, s, t), gate_kind, residual_scale,
         c.arg(grad_out, t, s), norm, eps, T, H, dtype, c.arg(grad_y, t, s), c.opt(grad_gamma, _FLOAT32, (H,)), c.opt(grad_beta, _FLOAT32, (H,)),
-        _gate(c, grad_gate, gate_kind, s, _FLOAT32 if gate_kind == MOE_GATE_CHANNEL else t), *c.workspace(workspace), c.stream))
+        _gate(c, grad_gate, gate_kind, s, _FLOAT32 if gate_kind == MOE_GATE_CHANNEL else t), *c.workspace(workspace), c.stream),
+        *_given(grad_y, grad_gamma, grad_beta, grad_gate))

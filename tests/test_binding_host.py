@@ -14,15 +14,10 @@ HUGE = [1 << 31, 1 << 32, (1 << 32) + 8, 1 << 40]      # 32 bits make a negative
 @pytest.fixture
 def no_device(monkeypatch):
     """Calls go through the binding with tensors that are on no device (their device is -1)."""
-    monkeypatch.setattr(binding, "_first_call", lambda: None)
-    monkeypatch.setattr(binding, "_INT32", torch.int32)
-    monkeypatch.setattr(binding, "_FLOAT32", torch.float32)
-    monkeypatch.setattr(binding, "_UINT8", torch.uint8)
+    binding._first_call()
     monkeypatch.setattr(binding, "_current_device", lambda: -1)
     monkeypatch.setattr(binding, "_raw_stream", lambda device: None)
     monkeypatch.setattr(binding, "_stream", lambda stream: None)
-    for t, number in ((torch.bfloat16, moe.MOE_BF16), (torch.float16, moe.MOE_FP16), (torch.float32, moe.MOE_FP32)):
-        monkeypatch.setitem(binding._DTYPES, t, number)
 
 
 def _t(*shape, dtype=torch.bfloat16):
@@ -115,7 +110,7 @@ def test_workspaces_and_plans_of_sizes_beyond_32_bits(value):
 
 def test_the_first_call_of_two_threads(monkeypatch):
     """Whenever another thread could look, between any two lines of the first call: what it takes for done is done."""
-    names = ["_INT32", "_FLOAT32", "_UINT8", "_current_device", "_raw_stream"]
+    names = ["_INT32", "_FLOAT32", "_UINT8", "_current_device", "_raw_stream", "_increment_version"]
     for name in names:
         monkeypatch.setattr(binding, name, None)
     monkeypatch.setattr(binding, "_DTYPES", {})
@@ -136,3 +131,60 @@ def test_the_first_call_of_two_threads(monkeypatch):
         sys.settrace(before)
     assert looks and all(looks)
     assert binding._INT32 is torch.int32
+
+
+def _all_arguments(T=0, H=64, E=8, k=2):
+    """(call, arguments by name, names of what it writes), every result wanted; the names are those of the call."""
+    ws = _t(1 << 20, dtype=torch.uint8)
+
+    def rows():
+        return _t(T, H)
+
+    def all_rows():
+        return _t(T * k, H)
+    pairs, gate = (T, k), moe.MOE_GATE_FULL
+    return [
+        (moe.moe_dispatch, dict(x=rows(), inv_perm=_i(*pairs), rows=all_rows()), "rows"),
+        (moe.moe_dispatch_backward, dict(grad_rows=all_rows(), inv_perm=_i(*pairs), grad_x=rows()), "grad_x"),
+        (moe.moe_combine, dict(rows=all_rows(), inv_perm=_i(*pairs), topk_weights=_f(*pairs), out=rows()), "out"),
+        (moe.moe_combine_backward, dict(grad_out=rows(), rows=all_rows(), inv_perm=_i(*pairs), topk_weights=_f(*pairs), grad_rows=all_rows(),
+                                        grad_weights=_f(*pairs)), "grad_rows grad_weights"),
+        (moe.moe_route_topk_backward, dict(topk_ids=_i(*pairs), topk_weights=_f(*pairs), grad_weights=_f(*pairs), grad_logits=_f(T, E)),
+         "grad_logits"),
+        (moe.moe_norm_before, dict(residual=rows(), update=rows(), residual_scale=1.0, gamma=_t(H), beta=_t(H), norm=0, eps=1e-5, sum=rows(),
+                                   x=rows()), "sum x"),
+        (moe.moe_norm_after, dict(residual=rows(), y=rows(), gamma=_t(H), beta=_t(H), gate=rows(), gate_kind=gate, residual_scale=1.0, norm=0,
+                                  eps=1e-5, out=rows()), "out"),
+        # without tokens these two would still clear sums on the device: none are wanted
+        (moe.moe_norm_before_backward, dict(sum=rows(), gamma=torch.empty(H, dtype=torch.bfloat16), grad_x=rows(), grad_sum=rows(), residual_scale=1.0,
+                                            norm=0, eps=1e-5, grad_residual=rows(), grad_update=rows(), grad_gamma=None, grad_beta=None,
+                                            workspace=ws), "grad_residual grad_update"),
+        (moe.moe_norm_after_backward, dict(y=rows(), gamma=torch.empty(H, dtype=torch.bfloat16), beta=_t(H), gate=rows(), gate_kind=gate,
+                                           residual_scale=1.0, grad_out=rows(), norm=0, eps=1e-5, grad_y=rows(), grad_gamma=None, grad_beta=None,
+                                           grad_gate=rows(), workspace=ws), "grad_y grad_gate"),
+    ]
+
+
+@pytest.mark.parametrize("case", _all_arguments(), ids=lambda case: case[0].__name__)
+def test_what_is_written_has_another_version(no_device, case):
+    call, args, outputs = case
+    tensors = {name: t for name, t in args.items() if isinstance(t, torch.Tensor)}
+    before = {name: t._version for name, t in tensors.items()}
+    call(**args)
+    changed = {name for name, t in tensors.items() if t._version != before[name]}
+    assert changed == set(outputs.split())
+    with pytest.raises(moe.MoEError):          # a refused call has written nothing
+        call(**args, stream=type("Stream", (), {"device_index": 0, "cuda_stream": None})())     # of another device
+    assert changed == {name for name, t in tensors.items() if t._version != before[name]} and all(
+        t._version == before[name] + 1 for name, t in tensors.items() if name in changed)
+    with torch.inference_mode():               # tensors without a version
+        call(**{name: torch.empty_like(t) if name in outputs.split() else t for name, t in args.items()})
+
+
+def test_a_gradient_that_needs_overwritten_rows(no_device):
+    """The stream is saved for the gradient of what follows, then a call in place takes it: no wrong gradient, but an error."""
+    h, w = _t(0, 64, dtype=torch.float32), torch.ones(64, device="meta", requires_grad=True)
+    loss = (h * w).sum()
+    moe.moe_norm_before(h, None, 1.0, _f(64), None, moe.MOE_NORM_RMS, 1e-5, h, _f(0, 64))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
