@@ -180,7 +180,12 @@ int moe_route_topk(const float *logits, int32_t T, int32_t E, int32_t k, int32_t
  * workspace: dev, >= moe_plan_workspace_bytes, 256-byte aligned; its index arrays stay readable until the
  * next forward on it.  seg_ready: dev uint32 [S] or NULL; segment s counts as arrived once
  * seg_ready[s] >= ready_epoch (written by whoever fills the segment, after the data); NULL = all
- * segments are ready.  act must equal the plan's.  Inputs are not modified. */
+ * segments are ready.  act must equal the plan's.  Inputs are not modified.
+ * With seg_ready the kernels wait on the GPU, so whatever writes the flags has to be able to run beside them.  A GPU writer needs room (option
+ * "n_cu") and a hardware queue of its own: HIP lays a process's streams on a few of these (4 by default, GPU_MAX_HW_QUEUES), and what is enqueued
+ * behind the forward on the same queue, though on another stream, starts when the forward ends -- after "spin_limit" polls, with MOE_ERR_TIMEOUT.
+ * A program that uses as many streams as there are queues, or more, enqueues the writer before the forward, or writes the flags from the host or
+ * another GPU. */
 int moe_layer_forward(moe_plan_t *plan, const void *x, const int32_t *topk_ids, const float *topk_weights,
                       const void *W1, const void *W2, int32_t act, void *out, void *workspace,
                       size_t workspace_bytes, const uint32_t *seg_ready, uint32_t ready_epoch, void *hip_stream);

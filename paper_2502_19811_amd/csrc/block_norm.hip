@@ -309,6 +309,10 @@ __global__ __launch_bounds__(threads_of<MW>()) void k_norm(NormParams p) {
 // to part_a and part_b, a row for each workgroup, which k_norm_columns adds up in a fixed order.  The next row is requested before the present one
 // is summed up (PRE), which the largest rows have no registers for.  Its loads are waited for by counting what was requested after them,
 // which takes that nothing is conditional: ALL says that the row is exact and that every optional row is given.
+// Rows of more than eight wavefronts leave a lane 128 registers, fewer than its sums, gamma and rows are in most variants for more than 8192
+// columns: those keep up to 248 bytes a lane in scratch memory, with four pieces up to 392.  us for 4096 rows of 8192 / 12288 / 16384 columns, without the sums of
+// columns: bf16 before 59 / 97 / 128 (5.7, 5.2, 5.3 TB/s), behind with a channel gate 35 / 64 / 80, with a full one 61 / 102 / 136, that with mean and
+// bias 63 / 177 / 230 (5.3, 2.8, 2.9 TB/s); fp32 before 123 / 220 / 346, channel 77 / 111 / 157, full 122 / 219 / 327, with mean and bias 134 / 359 / 459.
 enum { GRAD_BEFORE = 0, GRAD_AFTER = 1, GRAD_AFTER_TOKEN = 2, GRAD_AFTER_FULL = 3 };   // AFTER: no gate or a channel gate
 template <int DT, int MW, int NV, int MODE, bool WITH_B, bool PRE, bool ALL>
 __global__ __launch_bounds__(threads_of<MW>()) void k_norm_grad(NormGradParams p) {
@@ -567,9 +571,11 @@ namespace {
 uint32_t pieces_of(uint32_t row_bytes) { return (row_bytes + 15) / 16; }
 
 // Pieces a lane and wavefronts of a row.  One wavefront up to 128 pieces; then one piece a lane, or two where that makes rows of up to 512
-// pieces come out even; two beyond, four beyond 2048.  us for 1 / 512 / 16384 rows: 2048 columns (256 pieces) one wavefront 2.2 / 3.8 / 42.0, four 1.8 /
-// 3.4 / 42.4; 4096 columns one 3.4 / 5.7 / 94.1, four 2.4 / 4.8 / 89.5, eight 2.1 / 4.7 / 86.7 (8192 rows with the update: 41.0 with four, 42.9 with
-// eight); gradient of 4096 rows of 3584 columns four of two pieces, some of them empty, 30.0, seven of one 26.8.
+// pieces come out even; two beyond, four beyond 2048.  us in front of the block for 1 / 512 / 16384 rows: 2048 columns (256 pieces) one
+// wavefront of four pieces 2.2 / 3.8 / 42.0, four of one 1.9 / 3.4 / 42.6, two of two, which is taken, 2.1 / 3.5 / 41.8; 4096 columns one of eight
+// 3.4 / 5.7 / 94.1, eight of one 2.1 / 4.8 / 89.6, four of two, which is taken, 2.1 / 4.7 / 88.3 (8192 rows 41.5, eight of one 43.7).  The gradient
+// with the sums of columns: 2048 columns two of two 3.0 / 9.6 / 66.9, four of one 2.5 / 9.4 / 68.2; 4096 columns four of two 3.1 / 12.0 / 125, eight of
+// one 2.8 / 10.8 / 121; 4096 rows of 3584 columns four of two pieces, some of them empty, 30.0, seven of one 26.8.
 struct RowShape { int nv, waves; };
 RowShape shape_of(uint32_t pieces) {
   if (pieces <= 128) return {pieces <= 64 ? 1 : 2, 1};

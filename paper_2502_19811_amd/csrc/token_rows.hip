@@ -3,7 +3,8 @@
 //
 // With pairs q = t*k + j and e(q) the expert of pair q, the row of q is the number of pairs of lower experts plus the number of
 // its own expert's pairs before it; pairs without an expert have no row.  All of it is data movement: a row is read once and
-// written once, sums over a token's k rows and over a row's columns are fp32 in a fixed order.
+// written once (but a token's row for every slot in the gradient of a combine of more than 8), sums over a token's k rows and over a
+// row's columns are fp32 in a fixed order.
 #include "row_vector.h"
 
 namespace moe {
@@ -418,7 +419,8 @@ __global__ __launch_bounds__(LP == 64 ? kGradWaves * 64 : 256) void k_combine_gr
 // The weights of a token are the softmax of its kept logits, so d w_i / d logit_j = w_i (delta_ij - w_j) among them:
 // grad_logits[t][e] = sum over the slots j with expert e of w_j (g_j - sum_i g_i w_i).  A workgroup takes up to 1024 logits of whole tokens,
 // adds the slots in LDS, a thread a token in the order of j, and writes them in one piece.  (Every thread going through its token's slots
-// for 4 experts: 28.4 us for 65536 tokens of 256 experts, k = 8, so 20.7; 32768 of 64, k = 8 6.2 / 4.9; 32768 of 8, k = 2 2.6 / 3.0.)
+// for 4 experts: 28.4 us for 65536 tokens of 256 experts, k = 8, so 20.7; 32768 of 64, k = 8 6.2 / 4.9; 32768 of 8, k = 2 2.6 / 3.0.  These
+// find their inputs in the caches; where other work has run over them so takes 24.6, 5.7 and 4.6 to 5.1.)
 constexpr int kGateLogits = 1024;
 __global__ __launch_bounds__(256) void k_route_topk_grad(const int32_t* __restrict__ ids, const float* __restrict__ w,
                                                          const float* __restrict__ gw, int T, int E, int k, int tokens,
@@ -507,6 +509,10 @@ hipError_t combine_k(const RowCall& c, const void* rows, const int32_t* inv, con
     default: return combine_as<DT, K, 64, 2>(c, rows, inv, w, out);   // 1 or 4 pieces a lane are up to 5 % slower at one size or another
   }
 }
+// Slots whose rows are requested together: 1, 2, up to 4 or up to 8, whose two pieces a lane are 64 registers; more of them slot after slot
+// (K == 0).  us so / slot after slot, 16384 tokens of 2048 columns: k = 1 22.6 / 23.8, 2 32.6 / 32.9, 3
+// 43.5 / 44.8, 4 54.8 / 56.8, 5 67.0 / 68.6, 8 102 / 103; 48 tokens 2.5 / 2.7, 2.7 / 3.1, 2.6 / 3.2, 2.8 / 3.4, 3.3 / 3.8, 3.6 / 4.5.  Beyond 8: k = 9
+// 116, 10 128, 16 196, 32 376 (5.8 to 5.9 TB/s); 48 tokens 4.9, 5.4, 7.6, 16.2, an index and a row of latency a slot.
 template <int DT>
 hipError_t combine_type(const RowCall& c, const void* rows, const int32_t* inv, const float* w, void* out) {
   if (c.k == 1) return combine_k<DT, 1>(c, rows, inv, w, out);
@@ -546,6 +552,10 @@ hipError_t combine_grad_k(const RowCall& c, const void* g, const void* rows, con
       return combine_grad_as<DT, K, 64, 2>(c, g, rows, inv, w, grad_rows, grad_w);
   }
 }
+// Slots as in the combine; the token's row is loaded once for those that go together, and again for each of the others, with two barriers.
+// us so / slot after slot, 16384 tokens of 2048 columns: k = 1 37.0 / 37.3, 2 58.4 / 67.5, 3 86.6 / 105, 4 112 / 141, 5 138 / 176, 8 216 / 281; 48
+// tokens 3.1 / 3.2, 3.4 / 4.1, 3.8 / 4.9, 3.7 / 5.6, 4.5 / 6.6, 4.5 / 8.7.  Beyond 8: k = 9 326, 10 354, 16 567, 32 1117 (3.9 TB/s, against 5.3 with 8);
+// 48 tokens 9.7, 10.8, 16.9, 35.5.
 template <int DT>
 hipError_t combine_grad_type(const RowCall& c, const void* g, const void* rows, const int32_t* inv, const float* w, void* grad_rows, float* grad_w) {
   if (c.k == 1) return combine_grad_k<DT, 1>(c, g, rows, inv, w, grad_rows, grad_w);
