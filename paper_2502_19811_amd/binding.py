@@ -170,9 +170,10 @@ def moe_status_string(status: int) -> str:
 def moe_plan_create(T: int, H: int, F: int, E: int, k: int, S: int, act: int, seg_offsets: Sequence[int]) -> int:
     """Returns the plan handle.  seg_offsets: S+1 host integers."""
     lib = load_library()
-    _check_int32("moe_plan_create", T, H, F, E, k, S, act, *seg_offsets)
+    offsets = [int(v) for v in seg_offsets]
+    _check_int32("moe_plan_create", T, H, F, E, k, S, act, *offsets)
     shape = MoEShape(T, H, F, E, k, S, act)
-    seg = (C.c_int32 * (S + 1))(*[int(v) for v in seg_offsets])
+    seg = (C.c_int32 * (S + 1))(*offsets)
     handle = C.c_void_p()
     _check(lib.moe_plan_create(C.byref(handle), C.byref(shape), seg), "moe_plan_create")
     return handle.value

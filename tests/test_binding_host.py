@@ -91,6 +91,11 @@ def test_negative_numbers_of_experts(no_device):
         assert error.value.status == INVALID
 
 
+def test_plans_take_offsets_that_are_read_once():
+    for offsets in (iter([0, 40, 64]), (v for v in (0, 40, 64)), torch.tensor([0, 40, 64]), range(0, 65, 32)):
+        moe.moe_plan_destroy(moe.moe_plan_create(64, 256, 256, 8, 2, 2, moe.MOE_ACT_SWIGLU, offsets))
+
+
 @pytest.mark.parametrize("value", [*HUGE, -(1 << 32)])
 def test_workspaces_and_plans_of_sizes_beyond_32_bits(value):
     for at in range(3):
