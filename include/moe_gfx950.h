@@ -350,7 +350,8 @@ int moe_route_topk_backward(const int32_t *topk_ids, const float *topk_weights, 
 
 /* In front of the block: s = residual + residual_scale * update, sum = s, x = norm(s) * gamma + beta, with
  * norm(s) = s / sqrt(mean(s^2) + eps) (MOE_NORM_RMS) or (s - mean(s)) / sqrt(var(s) + eps) (MOE_NORM_LAYER), over the H columns.
- * x is normed from s before its rounding.  residual, update, sum, x: dev [T,H]; update NULL: s = residual; sum NULL: not wanted.
+ * x is normed from s before its rounding.  The squares are summed in fp32: |s| up to about 1e17, and where eps is 0 from 1e-18 on, where a row
+ * of zeros has no norm (NaN).  residual, update, sum, x: dev [T,H]; update NULL: s = residual; sum NULL: not wanted.
  * gamma, beta: dev [H] of the same type; beta NULL: none.  eps >= 0.  sum or x may be residual or update (in place). */
 int moe_norm_before(const void *residual, const void *update, float residual_scale, const void *gamma, const void *beta,
                     int32_t norm, float eps, int32_t T, int32_t H, int32_t dtype, void *sum, void *x, void *hip_stream);
